@@ -32,6 +32,7 @@
 #define BITCOS_GEMV_CUH
 
 #include "bitcos.h"
+#include "common.cuh"
 #include "decode.cuh"
 
 #include <cuda_runtime.h>
@@ -55,15 +56,12 @@ constexpr int kRows = BITCOS_TILE_ROWS;
 constexpr int kMaxWarps = 20;             // warps per thread block = tiles per item
 constexpr int kWarps16 = 14;              // the same for more than 8 tokens (16 warps per block: 128 registers per thread)
 constexpr int kMaxStages = 8;             // upper bound on the shared-memory ring depth (Plan::stages)
-constexpr uint64_t kWaitLimitNs = 500ull * 1000 * 1000;   // an mbarrier wait gives up after half a second
 constexpr int64_t kXResidentBytes = 48 * 1024;   // activations up to this size are kept in shared memory
 constexpr int kMmaMinBatch = 4;           // from this many tokens on the contraction runs on the tensor cores
 constexpr int kScrRowBytes = 48;          // a quarter of a decoded row (32 int8) + 16 bytes of padding against bank conflicts
 constexpr int kScrBytes = kRows * kScrRowBytes;   // per decoder warp: the transposition buffer in front of ldmatrix
 
 enum Format { kBitcos = 0, kTrit5 = 1, kBit2 = 2 };
-
-inline thread_local int g_last_cuda_error = 0;
 
 // The replicated lookup tables in their shared-memory form (decode.cuh); each thread block fetches
 // its copy from global memory with one bulk asynchronous copy.
@@ -421,14 +419,6 @@ __host__ __device__ inline SmemLayout smem_layout(int fmt, const Plan &pl, int G
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ float bf16_to_float(uint16_t b) { return __uint_as_float(static_cast<uint32_t>(b) << 16); }
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 // Bulk asynchronous copy global -> shared; size and both addresses are multiples of 16 bytes.
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
@@ -440,42 +430,6 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_
 __device__ __forceinline__ void bulk_prefetch_l2(const void *src, uint32_t bytes) {
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ uint64_t global_timer_ns() {
-    uint64_t t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-__device__ __forceinline__ uint32_t mbar_try(uint32_t bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return done;
-}
-// Polls until the phase completes, for at most limit_ns; false if it gave up.
-__device__ __forceinline__ bool mbar_wait_limited(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
-    uint64_t t0 = 0;
-    for (uint32_t i = 0;; ++i) {
-        if (mbar_try(bar, parity)) return true;
-        if ((i & 15u) == 15u) {
-            const uint64_t now = global_timer_ns();
-            if (t0 == 0) t0 = now;
-            else if (now - t0 > limit_ns) return false;
-        }
-    }
-}
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) { return mbar_wait_limited(bar, parity, kWaitLimitNs); }
-// Waits for the given phase parity (bounded); the common case, an already completed phase, costs
-// one instruction.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-    if (mbar_try(bar, parity)) return true;
-    return mbar_wait_slow(bar, parity);
-}
-
 // Four additions, packed in two instructions where that pays (with sixteen tokens pairs, and batches without guards, cost the
 // 32B-model layer 103.5 -> 106 us, in the 16-bit variant 8192x5120 at four tokens 11.30 -> 11.40).
 template <bool PACKED>
@@ -552,10 +506,6 @@ __device__ __forceinline__ int contract(const int (&w)[32], const int4 *xg, int 
 // Activation quantiser arithmetic (used by the quantiser kernels and by the products that take
 // 16-bit activations): a = max(max |x| over the group, 2^-100), scale = a / 127,
 // code = rint(x * (127 / a)), IEEE float32 quotient and product, ties to even.
-constexpr float kAmaxFloor = 7.888609052210118e-31f;      // 2^-100
-
-__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
 __device__ __forceinline__ uint32_t quant_code(float x, float inv) {
     int c = __float2int_rn(__fmul_rn(x, inv));
     c = c > 127 ? 127 : (c < -127 ? -127 : c);
@@ -779,10 +729,6 @@ __device__ __forceinline__ void mbar_arrive_lane0(uint32_t bar, int lane) {
         "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(lane)
         : "memory");
 }
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
 // A row block whose column blocks were split over several thread blocks: this block's share.
 struct Share {
     int rb;             // row block
@@ -2525,46 +2471,6 @@ __global__ void __launch_bounds__(max_block_threads(NB), 1) gemv_grouped_kernel(
 // ---------------------------------------------------------------------------------------------
 // Host side of the device entry points.
 // ---------------------------------------------------------------------------------------------
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-inline int check_cuda(cudaError_t e) {
-    if (e == cudaSuccess) return BITCOS_OK;
-    g_last_cuda_error = static_cast<int>(e);
-    return BITCOS_ERR_CUDA;
-}
-
-// Number of multiprocessors of the current device.  The opt-in to large dynamic shared memory is
-// done on the first call for a given kernel instantiation and device and remembered (so that
-// first call must not happen during stream capture; later calls only read the cache).
-template <auto kernel>
-int prepare_kernel(int *sms_out, int *smem_budget_out) {
-    constexpr int kMaxDev = 32;
-    static int cache[kMaxDev][2];      // [0] multiprocessor count (0 = not prepared yet), [1] dynamic smem budget
-    int dev = 0;
-    int rc = check_cuda(cudaGetDevice(&dev));
-    if (rc) return rc;
-    if (dev < kMaxDev && cache[dev][0] > 0) {
-        *sms_out = cache[dev][0];
-        *smem_budget_out = cache[dev][1];
-        return BITCOS_OK;
-    }
-    int sms = 0, max_smem = 0;
-    rc = check_cuda(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    if (rc) return rc;
-    rc = check_cuda(cudaDeviceGetAttribute(&max_smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev));
-    if (rc) return rc;
-    const int budget = max_smem - 1024;
-    rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, budget));
-    if (rc) return rc;
-    if (dev < kMaxDev) {
-        cache[dev][1] = budget;
-        cache[dev][0] = sms;
-    }
-    *sms_out = sms;
-    *smem_budget_out = budget;
-    return BITCOS_OK;
-}
-
 // Ring depth: as many stages as fit next to the tables, activations and partial sums (the loaded
 // DRAM latency of this part needs on the order of 100 KB in flight per multiprocessor).
 inline int choose_stages(int fmt, const Plan &pl, int G, int nb, int64_t K, int smem_budget, bool scr) {
@@ -2610,29 +2516,6 @@ inline void choose_walk(Plan &pl, int sms, int *grid) {
     *grid = static_cast<int>(cyclic ? g_cyc : g_con);
     pl.wq = cyclic ? 1 : static_cast<int>(pl.items / *grid);
     pl.wrem = cyclic ? 0 : static_cast<int>(pl.items - static_cast<int64_t>(pl.wq) * *grid);
-}
-
-// Launches with programmatic stream serialization, so that this kernel's prologue (barrier
-// set-up, table and first weight copies) may overlap the tail of the previous kernel in the
-// stream.  BITCOS_PDL=0 turns it off (for A/B runs).
-// (arguments of exactly the kernel's types, taken by reference: the largest are 7 KB, and every copy on the way counts
-// against launches of 2 us)
-template <typename... KArgs, typename... Args>
-int launch_pdl(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const Args &...args) {
-    static_assert(std::is_same<std::tuple<typename std::remove_cv<KArgs>::type...>, std::tuple<Args...>>::value, "the kernel's own types");
-    static const char *env = std::getenv("BITCOS_PDL");
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(static_cast<unsigned>(threads));
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = (env && env[0] == '0') ? 0 : 1;
-    void *pointers[] = {const_cast<void *>(static_cast<const void *>(&args))...};
-    return check_cuda(cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(kernel), pointers));
 }
 
 // While a launch sequence is being recorded for replay (bitcos_gemv_phases_host), every value a
