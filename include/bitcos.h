@@ -575,6 +575,70 @@ int bit2_gemv_grouped(const bitcos_weights *experts, int n_experts, int64_t M, i
                       int max_group_size, const int8_t *x, int n_xrows, const float *x_scale, float *y,
                       int32_t *acc_debug, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Around the experts' products of a mixture-of-experts layer: the router's choice, the grouping of
+ * pair lists of any length, and the sum over a token's experts.  (The paper runs its mixture-of-experts
+ * checkpoints, Table I, end to end only and gives no kernel for these.)  Stream ordered like the
+ * products; nothing is read or written before every earlier kernel in the stream has completed.
+ * ------------------------------------------------------------------------------------- */
+
+/* Element types of the entry points below. */
+typedef enum bitcos_type {
+    BITCOS_FP32 = 0,
+    BITCOS_BF16 = 1,
+    BITCOS_FP16 = 2
+} bitcos_type;
+
+/* A router's logits -> the experts of every token and their weights.
+ *     score   s = softmax(z) over the token's experts, or 1 / (1 + exp(-z)) each
+ *     choice  c = s + bias                                (the bias chooses, it does not weigh)
+ *     groups  the experts in n_groups runs of equal length; a group's value is the sum of its group_best (1 or 2) largest
+ *             choices; the top_groups groups with the largest values stay, equal values by index (n_groups = 1: all experts)
+ *     taken   the top_k experts with the largest choices, largest first, equal choices by index
+ *     weight  s, divided by (the sum of the token's taken s) + 1e-20 if renormalise != 0, times scale
+ * A logit or a bias that is NaN or -inf masks its expert: it is never taken (and in the softmax a masked logit counts
+ * nothing); +inf counts as the largest finite value.  Where fewer than top_k experts are left, the places behind them get
+ * expert -1 and weight 0: bitcos_group_pairs_device and bitcos_group_pairs_slots leave such pairs out.
+ * Which experts are taken is decided as in 64 bits: without a bias and without sums over two choices by the logits
+ * themselves (the order of exact scores), otherwise by c in 64 bits wherever 32 cannot tell.  The weights are formed in 32 bits.
+ *   logits       device [n_tokens] rows of n_experts values of logits_type, row_stride elements apart
+ *   bias         NULL or device float [n_experts]
+ *   n_tokens     0 is allowed (nothing is done); n_tokens * top_k at most 2^31 - 1; n_experts <= BITCOS_GROUP_EXPERTS_MAX
+ *   n_groups     at most 32, a divisor of n_experts; group_best at most n_experts / n_groups if n_groups > 1
+ *   top_k        1 .. BITCOS_ROUTE_TOP_K_MAX (more than n_experts: the last places get -1)
+ *   expert, weight   device int32 / float [n_tokens][top_k], overwritten
+ *   pair_xrow    device int32 [n_tokens * top_k], the token of every pair, as the grouping calls take it
+ * Pointers are aligned to their elements. */
+#define BITCOS_SCORE_SOFTMAX 0
+#define BITCOS_SCORE_SIGMOID 1
+#define BITCOS_ROUTE_TOP_K_MAX 32
+int bitcos_route_experts(const void *logits, int logits_type, int64_t row_stride, const float *bias, int n_tokens, int n_experts,
+                         int score, int n_groups, int top_groups, int group_best, int top_k, int renormalise, float scale,
+                         int32_t *expert, float *weight, int32_t *pair_xrow, void *cuda_stream);
+
+/* bitcos_group_pairs_device for lists of any length (a prompt's pairs), with every pair's place: the pairs are those of
+ * n_pairs / top_k tokens in order (pair i belongs to token i / top_k, which is what pair_xrow_sorted receives), and
+ *   slot   device int32 [n_pairs]: where pair i stands in the sorted lists (-1: left out, its expert is out of range) --
+ *          the row of the grouped products' outputs that bitcos_combine_pairs adds for it.
+ * The other lists as for bitcos_group_pairs_device, what the groups leave of them too: group_expert [min(n_pairs, n_experts)],
+ * group_begin [min(n_pairs, n_experts) + 1], pair_xrow_sorted, order [n_pairs], n_groups [1].  n_pairs 1 .. 2^31 - 1.
+ *   workspace   device scratch of bitcos_group_workspace_bytes(n_pairs, n_experts) bytes, contents of no matter before and
+ *               after; two calls that may run at the same time must not share it. */
+size_t bitcos_group_workspace_bytes(int64_t n_pairs, int n_experts);
+int bitcos_group_pairs_slots(const int32_t *pair_expert, int64_t n_pairs, int top_k, int n_experts, int32_t *group_expert,
+                             int32_t *group_begin, int32_t *pair_xrow_sorted, int32_t *order, int32_t *slot, int32_t *n_groups,
+                             void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* The sum over a token's experts:
+ *     out[t][m] = base[t][m] + sum over j of weight[t][j] * y[slot[t][j]][m]
+ * in 32 bits, j ascending (multiply-add), rounded once.  A slot outside [0, n_rows) adds nothing, whatever its weight.
+ *   y        device [n_rows][M] of y_type (BITCOS_FP32 or BITCOS_BF16), e.g. a grouped product's outputs
+ *   slot, weight   device int32 / float [n_tokens][top_k] (n_tokens 0: nothing is done)
+ *   base     NULL (zero) or device [n_tokens][M] of out_type, e.g. the residual; may be out itself
+ *   out      device [n_tokens][M] of out_type (BITCOS_FP32 or BITCOS_BF16); y, base and out 16-byte aligned */
+int bitcos_combine_pairs(const void *y, int y_type, int64_t n_rows, const int32_t *slot, const float *weight, int64_t n_tokens, int top_k,
+                         int64_t M, const void *base, void *out, int out_type, void *cuda_stream);
+
 #ifdef __GNUC__
 #pragma GCC visibility pop
 #endif

@@ -28,6 +28,7 @@ EXPORTED_SYMBOLS = [
     "bitcos_gemv_multi_host", "bitcos_quantize_activations", "bitcos_gemv_group_scales",
     "bitcos_choose_format", "bitcos_count_nnz_device", "bitcos_pack_device", "bitcos_pack_device_limited", "bitcos_gemv_bf16", "bitcos_gemv_multi_bf16",
     "bitcos_gemv_multi_group_scales", "bitcos_gemv_blend_bf16", "bitcos_decode_probe_variant", "bitcos_gemv_phased", "bitcos_gemv_phases_host", "trit5_gemv_grouped", "bit2_gemv_grouped", "bitcos_gemv_static_status", "bitcos_wait_probe", "bitcos_group_pairs_device", "bitcos_gemv_grouped_lists", "bitcos_gemv_multi_chained", "bitcos_gemv_multi_plan",
+    "bitcos_route_experts", "bitcos_group_workspace_bytes", "bitcos_group_pairs_slots", "bitcos_combine_pairs",
 ]
 
 
@@ -126,6 +127,11 @@ def load_library():
     L.bitcos_pack_device.argtypes = [vp, vp, i64, i64, vp, vp, sz, vp, vp, vp, C.POINTER(u64), vp, vp]
     L.bitcos_pack_device_limited.argtypes = [vp, vp, i64, i64, vp, vp, sz, vp, vp, vp, C.POINTER(u64), vp, u64, C.POINTER(C.c_int), vp]
     L.bitcos_gemv_group_scales.argtypes = [C.POINTER(_Weights), vp, vp, C.c_int, vp, vp, vp, sz, vp]
+    L.bitcos_route_experts.argtypes = [vp, C.c_int, i64, vp] + [C.c_int] * 8 + [C.c_float, vp, vp, vp, vp]
+    L.bitcos_group_workspace_bytes.restype = sz
+    L.bitcos_group_workspace_bytes.argtypes = [i64, C.c_int]
+    L.bitcos_group_pairs_slots.argtypes = [vp, i64, C.c_int, C.c_int, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.bitcos_combine_pairs.argtypes = [vp, C.c_int, i64, vp, vp, i64, C.c_int, i64, vp, vp, C.c_int, vp]
     _bind_calls(L)
     _lib = L
     return L
@@ -388,6 +394,18 @@ def _stream() -> int:
             _raw_stream = (lambda device: torch.cuda.current_stream(device).cuda_stream), torch.cuda.current_device
     stream, device = _raw_stream
     return stream(device())
+
+
+def _stream_of(*tensors) -> int:
+    """_stream(), for tensors that have to lie on the current device (None: an argument left out)."""
+    if _raw_stream is None:
+        _stream()
+    stream, device = _raw_stream
+    here = device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"tensors must be CUDA tensors on the current device ({here}), got one on {t.device}")
+    return stream(here)
 
 
 def make_workspace(M: int, K: int, device="cuda", copies: int = 1):
@@ -870,3 +888,109 @@ def bitcos_gemv_host(W: DeviceBitcos, x_host: np.ndarray, x_scale_host: np.ndarr
                                            y_host.ctypes.data, staging.data_ptr(), staging.numel(),
                                            workspace.data_ptr(), workspace.numel(), _stream()), "bitcos_gemv_host")
     return y_host
+
+
+# ---------------------------------------------------------------------------------------------
+# around the experts' products: routing, grouping of long lists, the sum over experts
+# ---------------------------------------------------------------------------------------------
+_SCORES = {"softmax": 0, "sigmoid": 1}
+_type_codes = None
+
+
+def _type_code(dtype, allowed, what):
+    """The library's number of a torch element type (bitcos_type)."""
+    global _type_codes
+    if _type_codes is None:
+        import torch
+        _type_codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    code = _type_codes.get(dtype, -1)
+    if code not in allowed:
+        raise ValueError(f"{what} cannot be {dtype}")
+    return code
+
+
+def _require(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def bitcos_route_experts(logits, top_k: int, bias=None, score: str = "softmax", n_groups: int = 1, top_groups: int = 1,
+                         group_best: int = 1, renormalise: bool = True, scale: float = 1.0):
+    """The router's choice: logits [tokens, experts] (float32, bfloat16 or float16, rows of unit stride) -> (expert int32
+    [tokens, top_k], weight float32 [tokens, top_k], pair_xrow int32 [tokens * top_k]).  score: "softmax" or "sigmoid"; bias
+    (float32 [experts]) is added for the choice only; of n_groups groups of experts the top_groups with the largest sums of
+    their group_best best choices are kept.  Masked experts (-inf or NaN) are never taken: expert -1, weight 0 where too few are left."""
+    import torch
+    _require(logits.dim() == 2 and logits.stride(1) == 1, "logits must be [tokens, experts] with rows of unit stride")
+    tokens, experts = logits.shape
+    _require(score in _SCORES, "score must be 'softmax' or 'sigmoid'")
+    _require(bias is None or (bias.dtype == torch.float32 and bias.shape == (experts,) and bias.is_contiguous()),
+             "bias must be a contiguous float32 [experts] tensor")
+    code = _type_code(logits.dtype, (0, 1, 2), "logits")
+    stream = _stream_of(logits, bias)
+    _require(1 <= top_k <= 32, "top_k must be 1 to 32")
+    out = torch.empty((3, tokens, top_k), dtype=torch.int32, device=logits.device)
+    expert, weight, xrow = out.unbind(0)
+    status = (_calls or _native()).bitcos_route_experts(
+        logits.data_ptr(), code, max(logits.stride(0), experts) if tokens <= 1 else logits.stride(0), 0 if bias is None else bias.data_ptr(),
+        tokens, experts, _SCORES[score], n_groups, top_groups, group_best, top_k, int(bool(renormalise)),
+        _float_bits(scale), expert.data_ptr(), weight.data_ptr(), xrow.data_ptr(), stream) if tokens else 0
+    if status:
+        _check(status, "bitcos_route_experts")
+    return expert, weight.view(torch.float32), xrow.view(-1)
+
+
+def _float_bits(v: float) -> int:
+    return C.c_int32.from_buffer(C.c_float(v)).value
+
+
+def make_group_workspace(n_pairs: int, n_experts: int, device="cuda"):
+    """Device scratch for bitcos_group_pairs_slots (any contents)."""
+    import torch
+    return torch.empty(int(load_library().bitcos_group_workspace_bytes(n_pairs, n_experts)), dtype=torch.uint8, device=device)
+
+
+def bitcos_group_pairs_slots(expert, n_experts: int, workspace=None):
+    """Groups the pairs of expert (int32 [tokens, top_k], as bitcos_route_experts returns it; any number of pairs) by expert:
+    returns (group_expert, group_begin, pair_xrow_sorted, order, slot, n_groups), device int32 tensors; slot [tokens, top_k] is every
+    pair's place in the sorted lists, -1 for pairs left out."""
+    import torch
+    _require(expert.dtype == torch.int32 and expert.dim() == 2 and expert.is_contiguous(), "expert must be a contiguous int32 [tokens, top_k] tensor")
+    tokens, top_k = expert.shape
+    P = tokens * top_k
+    stream = _stream_of(expert, workspace)
+    if workspace is None:
+        workspace = make_group_workspace(P, n_experts, expert.device)
+    cap = min(P, n_experts)
+    lists = torch.empty(2 * cap + 3 * P + 2, dtype=torch.int32, device=expert.device)
+    ge, gb, xr, order, slot, ng = lists.split((cap, cap + 1, P, P, P, 1))
+    status = (_calls or _native()).bitcos_group_pairs_slots(
+        expert.data_ptr(), P, top_k, n_experts, ge.data_ptr(), gb.data_ptr(), xr.data_ptr(), order.data_ptr(), slot.data_ptr(), ng.data_ptr(),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
+    if status:
+        _check(status, "bitcos_group_pairs_slots")
+    return ge, gb, xr, order, slot.view(tokens, top_k), ng
+
+
+def bitcos_combine_pairs(y, slot, weight, base=None, out=None, out_dtype=None):
+    """out[t] = base[t] + sum over j of weight[t, j] * y[slot[t, j]]: y [rows, M] (float32 or bfloat16), slot int32 and weight
+    float32 [tokens, top_k] (a slot outside the rows adds nothing), base and out [tokens, M] of one type (float32 or bfloat16;
+    out_dtype, else base's, else y's).  base may be out."""
+    import torch
+    _require(y.dim() == 2 and y.is_contiguous(), "y must be a contiguous [rows, M] tensor")
+    _require(slot.dtype == torch.int32 and slot.dim() == 2 and slot.is_contiguous(), "slot must be a contiguous int32 [tokens, top_k] tensor")
+    _require(weight.dtype == torch.float32 and weight.shape == slot.shape and weight.is_contiguous(), "weight must be contiguous float32, shaped as slot")
+    tokens, top_k = slot.shape
+    rows, M = y.shape
+    if out is None:
+        out = torch.empty((tokens, M), dtype=out_dtype or (y if base is None else base).dtype, device=y.device)
+    _require(out.shape == (tokens, M) and out.is_contiguous() and (out_dtype is None or out.dtype == out_dtype), "out must be a contiguous [tokens, M] tensor")
+    _require(base is None or (base.shape == out.shape and base.dtype == out.dtype and base.is_contiguous()), "base must be shaped and typed as out")
+    y_code, out_code = _type_code(y.dtype, (0, 1), "y"), _type_code(out.dtype, (0, 1), "out")
+    stream = _stream_of(y, slot, weight, base, out)
+    status = (_calls or _native()).bitcos_combine_pairs(
+        y.data_ptr(), y_code, rows, slot.data_ptr(), weight.data_ptr(), tokens, top_k, M, 0 if base is None else base.data_ptr(),
+        out.data_ptr(), out_code, stream) if tokens else 0
+    if status:
+        _check(status, "bitcos_combine_pairs")
+    return out

@@ -26,6 +26,13 @@ static int take(PyObject *const *args, Py_ssize_t n, Py_ssize_t want, const char
 #define I(i) ((int)v[i])
 #define Z(i) ((size_t)v[i])
 #define L(i) (v[i])
+static float as_float(int64_t bits) {
+    const int32_t b = (int32_t)bits;
+    float f;
+    memcpy(&f, &b, sizeof f);
+    return f;
+}
+#define F(i) as_float(v[i])      /* a float comes as the integer of its bits */
 #define TYPES(...) __VA_ARGS__
 #define CALL(name, count, types, ...)                                                       \
     static int (*p_##name)(types);                                                          \
@@ -88,12 +95,26 @@ CALL(bitcos_gemv_grouped_lists, 19,
      TYPES(void *, int, int64_t, int64_t, void *, void *, void *, int, void *, int, int, void *, int, void *, void *, void *, void *,
            size_t, void *),
      P(0), I(1), L(2), L(3), P(4), P(5), P(6), I(7), P(8), I(9), I(10), P(11), I(12), P(13), P(14), P(15), P(16), Z(17), P(18))
+/* (logits, type, row_stride, bias, n_tokens, n_experts, score, n_groups, top_groups, group_best, top_k, renormalise, scale, expert,
+   weight, pair_xrow, stream) */
+CALL(bitcos_route_experts, 17,
+     TYPES(void *, int, int64_t, void *, int, int, int, int, int, int, int, int, float, void *, void *, void *, void *), P(0), I(1), L(2),
+     P(3), I(4), I(5), I(6), I(7), I(8), I(9), I(10), I(11), F(12), P(13), P(14), P(15), P(16))
+/* (pair_expert, n_pairs, top_k, n_experts, group_expert, group_begin, pair_xrow_sorted, order, slot, n_groups, workspace,
+   workspace_bytes, stream) */
+CALL(bitcos_group_pairs_slots, 13,
+     TYPES(void *, int64_t, int, int, void *, void *, void *, void *, void *, void *, void *, size_t, void *), P(0), L(1), I(2), I(3),
+     P(4), P(5), P(6), P(7), P(8), P(9), P(10), Z(11), P(12))
+/* (y, y_type, n_rows, slot, weight, n_tokens, top_k, M, base, out, out_type, stream) */
+CALL(bitcos_combine_pairs, 12, TYPES(void *, int, int64_t, void *, void *, int64_t, int, int64_t, void *, void *, int, void *), P(0),
+     I(1), L(2), P(3), P(4), L(5), I(6), L(7), P(8), P(9), I(10), P(11))
 
 #define EVERY(X)                                                                                                           \
     X(bitcos_gemv) X(bitcos_gemv_group_scales) X(bitcos_gemv_bf16) X(bitcos_gemv_blend_bf16) X(trit5_gemv) X(bit2_gemv)    \
     X(bitcos_gemv_multi) X(bitcos_gemv_multi_bf16) X(bitcos_gemv_multi_group_scales) X(bitcos_gemv_multi_chained)          \
     X(bitcos_gemv_phases_host) X(bitcos_quantize_activations) X(bitcos_group_pairs_device) X(bitcos_gemv_grouped)          \
-    X(trit5_gemv_grouped) X(bit2_gemv_grouped) X(bitcos_gemv_grouped_lists)
+    X(trit5_gemv_grouped) X(bit2_gemv_grouped) X(bitcos_gemv_grouped_lists) X(bitcos_route_experts)                           \
+    X(bitcos_group_pairs_slots) X(bitcos_combine_pairs)
 
 /* bind(name, address): where the library's function is */
 static PyObject *bind(PyObject *self, PyObject *args) {

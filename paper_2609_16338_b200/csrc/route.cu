@@ -1,0 +1,730 @@
+// What stands around the experts' products of a mixture-of-experts layer, on the device:
+//   bitcos_route_experts       a router's logits -> the experts of every token and their weights
+//   bitcos_group_pairs_slots   the routed pairs sorted by expert (lists of any length), and every pair's place
+//   bitcos_combine_pairs       the experts' outputs weighted and added, token by token
+#include "bitcos.h"
+#include "common.cuh"
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cfloat>
+#include <climits>
+#include <cmath>
+
+using namespace bitcos_kernels;
+
+namespace {
+
+constexpr uint32_t kFull = 0xFFFFFFFFu;
+
+// ---------------------------------------------------------------------------------------------
+// Routing.  One warp per token; a lane holds V consecutive experts (expert = lane * V + v).
+//
+//   score  s = softmax(z) or 1 / (1 + exp(-z)),   choice c = s + bias
+//
+// Which expert is taken must not hang on how exp is rounded.  Without a bias (and without sums of scores for the groups)
+// the order of the scores is the order of the logits, and that is what is compared.  Otherwise c is formed in 32 bits with
+// a bound on its error; where two choices whose order matters lie closer than their bounds, the warp does the
+// token once more in 64 bits (route_exact).
+// ---------------------------------------------------------------------------------------------
+constexpr int kRouteWarps = 4;
+constexpr int kMaxRouteGroups = 32;
+
+struct RouteArgs {
+    const void *logits;
+    const float *bias;          // NULL: none
+    int64_t row_stride;         // elements
+    int32_t *expert;            // [tokens][top_k]
+    int32_t *xrow;              // [tokens * top_k]
+    float *weight;              // [tokens][top_k]
+    float scale;
+    int tokens, experts, top_k;
+    int n_groups, top_groups, group_best, group_size;
+    int softmax, renormalise, by_choice;   // by_choice: the order of c, else of the logits
+    int vector;                 // rows may be read V values at a time
+};
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+
+// a value -> an unsigned with the same order; 0 stands for "not to be taken" (below every finite value's)
+__device__ __forceinline__ uint32_t ordered(float v) {
+    const uint32_t b = __float_as_uint(v);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, d));
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ T warp_sum(T v) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(kFull, v, d);
+    return v;
+}
+
+// A logit as it counts: +inf as the largest finite value, -inf and NaN as masked (-inf), -0 as 0.
+__device__ __forceinline__ float clean(float z) {
+    if (!(z > -INFINITY)) return -INFINITY;
+    return fminf(z, FLT_MAX) + 0.0f;
+}
+
+// The two largest of a stream of values.
+template <typename T>
+struct Two {
+    T a, b;
+    __device__ __forceinline__ void add(T v) {
+        if (v > a) {
+            b = a;
+            a = v;
+        } else if (v > b) {
+            b = v;
+        }
+    }
+};
+
+// The whole token in 64 bits: lane j < top_k gets the expert of place j (-1: none is left).  Rare, so short rather than fast.
+template <int V, typename L>
+__device__ __noinline__ int route_exact(const RouteArgs &a, const L *row, int lane) {
+    double c[V];
+    double top = -INFINITY, sum = 0.0;
+    for (int v = 0; v < V; ++v) {
+        const int e = lane * V + v;
+        c[v] = e < a.experts ? static_cast<double>(clean(to_float(row[e]))) : -INFINITY;
+        top = fmax(top, c[v]);
+    }
+    if (a.softmax) {
+        for (int d = 16; d; d >>= 1) top = fmax(top, __shfl_xor_sync(kFull, top, d));
+        for (int v = 0; v < V; ++v) sum += c[v] > -INFINITY ? exp(c[v] - top) : 0.0;
+        sum = warp_sum(sum);
+    }
+    for (int v = 0; v < V; ++v) {
+        const int e = lane * V + v;
+        if (!(c[v] > -INFINITY)) continue;
+        const double s = a.softmax ? exp(c[v] - top) / sum : 1.0 / (1.0 + exp(-c[v]));
+        const float b = a.bias ? clean(a.bias[e]) : 0.0f;
+        c[v] = s + static_cast<double>(b);
+    }
+    if (a.n_groups > 1) {
+        double mine = -INFINITY;                             // lane g: the value of group g
+        for (int g = 0; g < a.n_groups; ++g) {
+            Two<double> t{-INFINITY, -INFINITY};
+            for (int v = 0; v < V; ++v)
+                if ((lane * V + v) / a.group_size == g && lane * V + v < a.experts) t.add(c[v]);
+            for (int d = 16; d; d >>= 1) {
+                const double oa = __shfl_xor_sync(kFull, t.a, d), ob = __shfl_xor_sync(kFull, t.b, d);
+                t.b = fmax(fmin(t.a, oa), fmax(t.b, ob));
+                t.a = fmax(t.a, oa);
+            }
+            const double value = a.group_best == 2 ? t.a + t.b : t.a;
+            if (lane == g) mine = value;
+        }
+        int ahead = 0;
+        for (int g = 0; g < a.n_groups; ++g) {
+            const double other = __shfl_sync(kFull, mine, g);
+            ahead += other > mine || (other == mine && g < lane);
+        }
+        const uint32_t kept = __ballot_sync(kFull, lane < a.n_groups && ahead < a.top_groups);
+        for (int v = 0; v < V; ++v) {
+            const int e = lane * V + v;
+            if (e >= a.experts || !((kept >> (e / a.group_size)) & 1u)) c[v] = -INFINITY;
+        }
+    }
+    int taken = -1;
+    for (int j = 0; j < a.top_k; ++j) {
+        double best = -INFINITY;
+        int at = INT_MAX;
+        for (int v = 0; v < V; ++v)
+            if (c[v] > best) {
+                best = c[v];
+                at = lane * V + v;
+            }
+        for (int d = 16; d; d >>= 1) {
+            const double ob = __shfl_xor_sync(kFull, best, d);
+            const int oat = __shfl_xor_sync(kFull, at, d);
+            if (ob > best || (ob == best && oat < at)) {
+                best = ob;
+                at = oat;
+            }
+        }
+        if (at == INT_MAX) break;                            // (the same on every lane)
+        for (int v = 0; v < V; ++v)
+            if (lane * V + v == at) c[v] = -INFINITY;
+        if (lane == j) taken = at;
+    }
+    return taken;
+}
+
+template <int V, typename L>
+__global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const __grid_constant__ RouteArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5);
+    if (token >= a.tokens) return;
+    const L *row = static_cast<const L *>(a.logits) + token * a.row_stride;
+    float z[V];
+    if (a.vector) {
+        constexpr int kBytes = V * sizeof(L) < 16 ? V * sizeof(L) : 16;
+        constexpr int kPer = kBytes / sizeof(L);
+#pragma unroll
+        for (int i = 0; i < V / kPer; ++i) {
+            alignas(16) L part[kPer];
+            const char *src = reinterpret_cast<const char *>(row + lane * V + i * kPer);
+            if constexpr (kBytes == 16) *reinterpret_cast<uint4 *>(part) = *reinterpret_cast<const uint4 *>(src);
+            else if constexpr (kBytes == 8) *reinterpret_cast<uint2 *>(part) = *reinterpret_cast<const uint2 *>(src);
+            else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t *>(part) = *reinterpret_cast<const uint32_t *>(src);
+            else *reinterpret_cast<uint16_t *>(part) = *reinterpret_cast<const uint16_t *>(src);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) z[i * kPer + j] = clean(to_float(part[j]));
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = lane * V + v;
+            z[v] = e < a.experts ? clean(to_float(row[e])) : -INFINITY;
+        }
+    }
+    float top = 0.f, sum = 1.f;
+    if (a.softmax) {
+        top = z[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) top = fmaxf(top, z[v]);
+        top = warp_max(top);
+        sum = 0.f;
+        if (top > -INFINITY) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum += expf(z[v] - top);      // (a masked one: exp(-inf) = 0)
+        }
+        sum = warp_sum(sum);
+    }
+    const auto score = [&](float zz) { return a.softmax ? expf(zz - top) / sum : 1.0f / (1.0f + expf(-zz)); };
+    // bound on the error of a score s of logit zz, and with it of the choice c = s + b: exp, sum and quotient are good to
+    // 2^-20 of s, the argument's rounding adds 2^-24 of itself, the addition 2^-24 of c (bounds doubled; 1e-38: scores below the normal
+    // range, which exp may have rounded to nothing)
+    const auto error = [&](float s, float zz, float c) {
+        const float d = a.softmax ? fminf(top - zz, 128.f) : 0.f;
+        return s * (9.5367431640625e-7f + d * 1.1920929e-7f) + fabsf(c) * 1.1920929e-7f + 1e-38f;
+    };
+
+    uint32_t key[V];
+    float upper[V];                // the choice with its bound added (by_choice only)
+    bool near = false;             // an order that 32 bits cannot tell
+    if (!a.by_choice) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) key[v] = z[v] > -INFINITY ? ordered(z[v]) : 0u;
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = lane * V + v;
+            key[v] = 0u;
+            upper[v] = -INFINITY;
+            if (z[v] > -INFINITY) {
+                const float b = a.bias ? clean(__ldg(a.bias + e)) : 0.f;
+                if (b > -INFINITY) {
+                    const float s = score(z[v]), c = fminf(s + b, FLT_MAX) + 0.0f;
+                    key[v] = ordered(c);
+                    upper[v] = c + error(s, z[v], c);
+                }
+            }
+        }
+    }
+
+    if (a.n_groups > 1) {
+        // lane g: the value of group g, and how far it may be off
+        float mine = -INFINITY, off = 0.f;
+        for (int g = 0; g < a.n_groups; ++g) {
+            Two<float> t{-INFINITY, -INFINITY};
+            float far = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int e = lane * V + v;
+                if (key[v] && e / a.group_size == g) {
+                    const float c = unordered(key[v]);
+                    t.add(c);
+                    if (a.by_choice) far = fmaxf(far, upper[v] - c);
+                }
+            }
+#pragma unroll
+            for (int d = 16; d; d >>= 1) {
+                const float oa = __shfl_xor_sync(kFull, t.a, d), ob = __shfl_xor_sync(kFull, t.b, d);
+                far = fmaxf(far, __shfl_xor_sync(kFull, far, d));
+                t.b = fmaxf(fminf(t.a, oa), fmaxf(t.b, ob));
+                t.a = fmaxf(t.a, oa);
+            }
+            const float value = a.group_best == 2 ? t.a + t.b : t.a;
+            if (lane == g) {
+                mine = value;
+                off = value > -INFINITY ? 2.f * far + fabsf(value) * 1.1920929e-7f : 0.f;
+            }
+        }
+        int ahead = 0;
+        for (int g = 0; g < a.n_groups; ++g) {
+            const float other = __shfl_sync(kFull, mine, g);
+            ahead += other > mine || (other == mine && g < lane);
+        }
+        const bool is_group = lane < a.n_groups, keep = is_group && ahead < a.top_groups;
+        const uint32_t kept = __ballot_sync(kFull, keep);
+        if (a.by_choice && a.top_groups < a.n_groups) {
+            const float low = -warp_max(keep ? off - mine : -INFINITY);
+            const float high = warp_max(is_group && !keep ? mine + off : -INFINITY);
+            near = high > -INFINITY && high >= low;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int e = lane * V + v;
+            if (e < a.experts && !((kept >> (e / a.group_size)) & 1u)) {
+                key[v] = 0u;
+                upper[v] = -INFINITY;
+            }
+        }
+    }
+
+    int taken = -1;                // lane j: the expert of place j
+    uint32_t taken_key = 0u;
+    int places = a.top_k;          // how many were found
+    for (int j = 0; j < a.top_k; ++j) {
+        uint32_t best = key[0];
+        int at = 0;
+#pragma unroll
+        for (int v = 1; v < V; ++v)
+            if (key[v] > best) {
+                best = key[v];
+                at = v;
+            }
+        const uint32_t all = __reduce_max_sync(kFull, best);
+        if (all == 0u) {
+            places = j;
+            break;
+        }
+        const int winner = __ffs(__ballot_sync(kFull, best == all)) - 1;      // (lowest lane = lowest expert)
+        const int e = __shfl_sync(kFull, lane * V + at, winner);
+        if (lane == winner) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v == at) {
+                    key[v] = 0u;
+                    if (a.by_choice) upper[v] = -INFINITY;
+                }
+        }
+        if (lane == j) {
+            taken = e;
+            taken_key = all;
+        }
+    }
+
+    float zt = taken >= 0 ? clean(to_float(row[taken])) : -INFINITY;
+    float s = taken >= 0 ? score(zt) : 0.f;
+    if (a.by_choice) {
+        // the taken choices in order, every one above the next by more than their bounds (or the same logit and bias, where
+        // the lower index goes first), the last one above all that are left
+        const float c = taken >= 0 ? unordered(taken_key) : 0.f;
+        const float b = taken >= 0 && a.bias ? clean(__ldg(a.bias + taken)) : 0.f;
+        const float err = error(s, zt, c);
+        const float up_next = __shfl_down_sync(kFull, c + err, 1), z_next = __shfl_down_sync(kFull, zt, 1), b_next = __shfl_down_sync(kFull, b, 1);
+        bool close = lane + 1 < places && up_next >= c - err && !(z_next == zt && b_next == b);
+        if (places == a.top_k) {
+            float left = upper[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) left = fmaxf(left, upper[v]);
+            left = warp_max(left);
+            close = close || (lane == places - 1 && left >= c - err && left > -INFINITY);
+        }
+        near = near || __any_sync(kFull, close);
+        if (near) {
+            taken = route_exact<V, L>(a, row, lane);
+            zt = taken >= 0 ? clean(to_float(row[taken])) : -INFINITY;
+            s = taken >= 0 ? score(zt) : 0.f;
+        }
+    }
+    if (a.renormalise) s = s / (warp_sum(s) + 1e-20f);
+    if (lane < a.top_k) {
+        const int64_t p = token * a.top_k + lane;
+        a.expert[p] = taken;
+        a.weight[p] = s * a.scale;
+        a.xrow[p] = static_cast<int32_t>(token);
+    }
+}
+
+template <int V, typename L>
+int launch_route(const RouteArgs &a, cudaStream_t stream) {
+    const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(a.tokens) + kRouteWarps - 1) / kRouteWarps);
+    return launch_pdl(route_kernel<V, L>, dim3(blocks), kRouteWarps * 32, 0, stream, a);
+}
+
+template <typename L>
+int launch_route_type(RouteArgs a, cudaStream_t stream) {
+    int V = 1;
+    while (V * 32 < a.experts) V *= 2;
+    const size_t chunk = std::min<size_t>(16, V * sizeof(L));
+    a.vector = a.experts == V * 32 && reinterpret_cast<uintptr_t>(a.logits) % chunk == 0 && a.row_stride * sizeof(L) % chunk == 0;
+    switch (V) {
+        case 1: return launch_route<1, L>(a, stream);
+        case 2: return launch_route<2, L>(a, stream);
+        case 4: return launch_route<4, L>(a, stream);
+        case 8: return launch_route<8, L>(a, stream);
+        case 16: return launch_route<16, L>(a, stream);
+        default: return launch_route<32, L>(a, stream);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Pairs sorted by expert, lists of any length: a stable counting sort.  The list is cut into one chunk per block, a
+// chunk into one run per warp.  With several blocks a first kernel counts every chunk's pairs per expert; then each block
+// knows what lies in front of its own (all experts before, the same expert's pairs in earlier chunks), counts its runs, and its
+// warps place their runs 32 pairs at a time (match_any: the earlier lanes with the same expert).
+// ---------------------------------------------------------------------------------------------
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortMaxBlocks = 148;
+constexpr int64_t kSortOneBlock = 4096;      // up to this many pairs one block does everything
+
+struct SortArgs {
+    const int32_t *pair_expert;
+    int32_t *group_expert, *group_begin, *xrow, *order, *slot, *n_groups;
+    int32_t *counts;            // [blocks][experts], what count_kernel found
+    int n_pairs, n_experts, top_k;
+    int chunk;                  // pairs per block, a multiple of 32
+};
+
+inline int sort_blocks(int64_t n_pairs) {
+    return n_pairs <= kSortOneBlock ? 1 : static_cast<int>(std::min<int64_t>(kSortMaxBlocks, (n_pairs + 1023) / 1024));
+}
+
+template <typename T>
+__device__ __forceinline__ T smaller(T a, T b) {
+    return a < b ? a : b;
+}
+
+__global__ void __launch_bounds__(kSortThreads) count_kernel(const __grid_constant__ SortArgs a) {
+    extern __shared__ int32_t count[];
+    for (int e = threadIdx.x; e < a.n_experts; e += blockDim.x) count[e] = 0;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __syncthreads();
+    const int64_t from = static_cast<int64_t>(blockIdx.x) * a.chunk;
+    const int64_t to = smaller<int64_t>(a.n_pairs, from + a.chunk);
+    for (int64_t i = from + threadIdx.x; i < to; i += blockDim.x) {
+        const int e = __ldg(a.pair_expert + i);
+        if (e >= 0 && e < a.n_experts) atomicAdd(count + e, 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.n_experts; e += blockDim.x) a.counts[static_cast<int64_t>(blockIdx.x) * a.n_experts + e] = count[e];
+}
+
+__global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_constant__ SortArgs a) {
+    extern __shared__ int32_t shared[];
+    const int E = a.n_experts, warps = blockDim.x >> 5;
+    int32_t *run = shared;                       // [warps][E]: pairs of a run per expert, then the run's next free place
+    int32_t *start = shared + warps * E;         // [E]: where this block's pairs of an expert go
+    int32_t *total = start + E;                  // [E]: all pairs of an expert
+    __shared__ int32_t warp_pairs[kSortWarps], warp_groups[kSortWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    for (int i = tid; i < warps * E; i += blockDim.x) run[i] = 0;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __syncthreads();
+    // this warp's run: whole rounds of 32 pairs
+    const int64_t from = static_cast<int64_t>(blockIdx.x) * a.chunk;
+    const int64_t to = smaller<int64_t>(a.n_pairs, from + a.chunk);
+    const int rounds = static_cast<int>((to - from + 31) / 32), per = (rounds + warps - 1) / warps;
+    const int64_t mine = from + static_cast<int64_t>(warp) * per * 32;
+    const int64_t mine_end = smaller<int64_t>(to, mine + static_cast<int64_t>(per) * 32);
+    int32_t *next = run + warp * E;
+    for (int64_t i = mine + lane; i < mine_end; i += 32) {
+        const int e = __ldg(a.pair_expert + i);
+        if (e >= 0 && e < E) atomicAdd(next + e, 1);
+    }
+    __syncthreads();
+    // an expert's pairs in this block's earlier runs, and in all if there is no other block
+    for (int e = tid; e < E; e += blockDim.x) {
+        int sum = 0;
+        for (int w = 0; w < warps; ++w) {
+            const int n = run[w * E + e];
+            run[w * E + e] = sum;
+            sum += n;
+        }
+        start[e] = 0;
+        total[e] = gridDim.x > 1 ? 0 : sum;
+    }
+    __syncthreads();
+    if (gridDim.x > 1) {
+        // in earlier blocks, and in all: the blocks' counts are shared out over the threads (whole numbers: any order will do)
+        const int parts = static_cast<int>(blockDim.x) > E ? static_cast<int>(blockDim.x) / E : 1, blocks = gridDim.x, each = (blocks + parts - 1) / parts;
+        for (int i = tid; i < parts * E; i += blockDim.x) {
+            const int e = i % E, b0 = i / E * each, b1 = smaller(blocks, b0 + each);
+            int before = 0, all = 0;
+#pragma unroll 8
+            for (int b = b0; b < b1; ++b) {
+                const int n = a.counts[static_cast<int64_t>(b) * E + e];
+                if (b < static_cast<int>(blockIdx.x)) before += n;
+                all += n;
+            }
+            if (before) atomicAdd(start + e, before);
+            if (all) atomicAdd(total + e, all);
+        }
+        __syncthreads();
+    }
+    // experts in order: the pairs and the groups in front of each (blockDim.x experts a round)
+    int pairs_before = 0, groups_before = 0;
+    for (int base = 0; base < E; base += blockDim.x) {
+        const int e = base + tid;
+        const int n = e < E ? total[e] : 0;
+        int p = n, g = n > 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int up = __shfl_up_sync(kFull, p, d), ug = __shfl_up_sync(kFull, g, d);
+            if (lane >= d) {
+                p += up;
+                g += ug;
+            }
+        }
+        if (lane == 31) {
+            warp_pairs[warp] = p;
+            warp_groups[warp] = g;
+        }
+        __syncthreads();
+        int all_pairs = 0, all_groups = 0;
+        for (int w = 0; w < warps; ++w) {
+            if (w == warp) {
+                p += all_pairs;
+                g += all_groups;
+            }
+            all_pairs += warp_pairs[w];
+            all_groups += warp_groups[w];
+        }
+        if (e < E) {
+            const int at = pairs_before + p - n, group = groups_before + g - (n > 0);
+            start[e] += at;
+            if (n > 0 && blockIdx.x == 0) {
+                a.group_expert[group] = e;
+                a.group_begin[group] = at;
+            }
+        }
+        pairs_before += all_pairs;
+        groups_before += all_groups;
+        __syncthreads();
+    }
+    const int cap = smaller(a.n_pairs, E);
+    if (blockIdx.x == 0) {
+        for (int g = groups_before + tid; g <= cap; g += blockDim.x) {
+            a.group_begin[g] = g == groups_before ? pairs_before : 0;
+            if (g < cap) a.group_expert[g] = 0;
+        }
+        if (tid == 0) *a.n_groups = groups_before;
+    }
+    for (int64_t i = pairs_before + static_cast<int64_t>(blockIdx.x) * blockDim.x + tid; i < a.n_pairs; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        a.xrow[i] = 0;
+        a.order[i] = -1;
+    }
+    for (int64_t base = mine; base < mine_end; base += 32) {
+        const int64_t i = base + lane;
+        int e = i < mine_end ? __ldg(a.pair_expert + i) : -1;
+        if (e < 0 || e >= E) e = -1;
+        const uint32_t same = __match_any_sync(kFull, e);
+        const int at = e >= 0 ? start[e] + next[e] + __popc(same & ((1u << lane) - 1u)) : -1;
+        __syncwarp();
+        if (e >= 0 && lane == __ffs(same) - 1) next[e] += __popc(same);
+        __syncwarp();
+        if (i < mine_end) a.slot[i] = at;
+        if (at >= 0) {
+            a.order[at] = static_cast<int32_t>(i);
+            a.xrow[at] = static_cast<int32_t>(i / a.top_k);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// out[t] = base[t] + sum over j of weight[t][j] * y[slot[t][j]], j ascending, in 32 bits; a thread takes W neighbouring
+// columns of one token, reads up to eight experts' values before it adds the first, and rounds once.
+// Bound by memory: every y row is read once.
+// ---------------------------------------------------------------------------------------------
+struct CombineArgs {
+    const void *y;
+    const int32_t *slot;
+    const float *weight;
+    const void *base;           // NULL: none; the output's type
+    void *out;
+    int64_t chunks;             // tokens * (M / W)
+    int64_t M;
+    int64_t n_rows;             // rows of y
+    int per_row;                // M / W
+    int top_k;
+};
+
+template <typename T, int W>
+struct alignas(sizeof(T) * W < 16 ? sizeof(T) * W : 16) Pack {
+    T v[W];
+};
+__device__ __forceinline__ void from_float(float v, float &o) { o = v; }
+__device__ __forceinline__ void from_float(float v, __nv_bfloat16 &o) { o = __float2bfloat16_rn(v); }
+
+template <typename Y, typename O, int W>
+__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ CombineArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t chunk = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    if (chunk >= a.chunks) return;
+    const int64_t token = chunk / a.per_row;
+    const int64_t column = (chunk - token * a.per_row) * W;
+    float acc[W];
+    if (a.base) {
+        const Pack<O, W> b = *reinterpret_cast<const Pack<O, W> *>(static_cast<const O *>(a.base) + token * a.M + column);
+#pragma unroll
+        for (int i = 0; i < W; ++i) acc[i] = to_float(b.v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) acc[i] = 0.f;
+    }
+    const int32_t *slot = a.slot + token * a.top_k;
+    const float *weight = a.weight + token * a.top_k;
+    const Y *y = static_cast<const Y *>(a.y) + column;
+    constexpr int kBatch = 8;
+    for (int j0 = 0; j0 < a.top_k; j0 += kBatch) {
+        Pack<Y, W> part[kBatch];
+        float w[kBatch];
+        bool there[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int64_t r = j0 + j < a.top_k ? __ldg(slot + j0 + j) : -1;
+            there[j] = r >= 0 && r < a.n_rows;
+            if (there[j]) {
+                w[j] = __ldg(weight + j0 + j);
+                part[j] = *reinterpret_cast<const Pack<Y, W> *>(y + r * a.M);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (there[j]) {
+#pragma unroll
+                for (int i = 0; i < W; ++i) acc[i] = fmaf(w[j], to_float(part[j].v[i]), acc[i]);
+            }
+    }
+    Pack<O, W> o;
+#pragma unroll
+    for (int i = 0; i < W; ++i) from_float(acc[i], o.v[i]);
+    *reinterpret_cast<Pack<O, W> *>(static_cast<O *>(a.out) + token * a.M + column) = o;
+}
+
+template <typename Y, typename O, int W>
+int launch_combine_wide(CombineArgs a, int64_t tokens, cudaStream_t stream) {
+    a.per_row = static_cast<int>(a.M / W);
+    a.chunks = tokens * a.per_row;
+    const int64_t blocks = (a.chunks + 255) / 256;
+    if (blocks > INT_MAX) return BITCOS_ERR_SHAPE;
+    return launch_pdl(combine_kernel<Y, O, W>, dim3(static_cast<unsigned>(blocks)), 256, 0, stream, a);
+}
+
+template <typename Y, typename O>
+int launch_combine(const CombineArgs &a, int64_t tokens, cudaStream_t stream) {
+    // whole 16-byte loads of y where the rows allow them (rows are M elements apart, all pointers are 16-byte aligned)
+    constexpr int kMost = 16 / sizeof(Y);
+    if (a.M % kMost == 0) return launch_combine_wide<Y, O, kMost>(a, tokens, stream);
+    if (a.M % 2 == 0) return launch_combine_wide<Y, O, 2>(a, tokens, stream);
+    return launch_combine_wide<Y, O, 1>(a, tokens, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int bitcos_route_experts(const void *logits, int logits_type, int64_t row_stride, const float *bias, int n_tokens, int n_experts,
+                         int score, int n_groups, int top_groups, int group_best, int top_k, int renormalise, float scale,
+                         int32_t *expert, float *weight, int32_t *pair_xrow, void *cuda_stream) {
+    if (!logits || !expert || !weight || !pair_xrow) return BITCOS_ERR_NULL;
+    if (n_tokens < 0 || n_experts < 1 || n_experts > BITCOS_GROUP_EXPERTS_MAX || row_stride < n_experts) return BITCOS_ERR_SHAPE;
+    if (top_k < 1 || top_k > BITCOS_ROUTE_TOP_K_MAX || static_cast<int64_t>(n_tokens) * top_k > INT_MAX) return BITCOS_ERR_SHAPE;
+    if (score != BITCOS_SCORE_SOFTMAX && score != BITCOS_SCORE_SIGMOID) return BITCOS_ERR_SHAPE;
+    if (n_groups < 1 || n_groups > kMaxRouteGroups || n_experts % n_groups != 0 || top_groups < 1 || top_groups > n_groups)
+        return BITCOS_ERR_SHAPE;
+    if (group_best < 1 || group_best > 2 || (n_groups > 1 && group_best > n_experts / n_groups)) return BITCOS_ERR_SHAPE;
+    if (logits_type != BITCOS_FP32 && logits_type != BITCOS_BF16 && logits_type != BITCOS_FP16) return BITCOS_ERR_SHAPE;
+    const size_t size = logits_type == BITCOS_FP32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % size || reinterpret_cast<uintptr_t>(bias) % 4 || reinterpret_cast<uintptr_t>(expert) % 4 ||
+        reinterpret_cast<uintptr_t>(weight) % 4 || reinterpret_cast<uintptr_t>(pair_xrow) % 4)
+        return BITCOS_ERR_ALIGN;
+    if (n_tokens == 0) return BITCOS_OK;
+    RouteArgs a{};
+    a.logits = logits;
+    a.bias = bias;
+    a.row_stride = row_stride;
+    a.expert = expert;
+    a.weight = weight;
+    a.xrow = pair_xrow;
+    a.scale = scale;
+    a.tokens = n_tokens;
+    a.experts = n_experts;
+    a.top_k = top_k;
+    a.n_groups = n_groups;
+    a.top_groups = top_groups;
+    a.group_best = group_best;
+    a.group_size = n_experts / n_groups;
+    a.softmax = score == BITCOS_SCORE_SOFTMAX;
+    a.renormalise = renormalise != 0;
+    a.by_choice = bias != nullptr || (n_groups > 1 && group_best == 2);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (logits_type == BITCOS_FP32) return launch_route_type<float>(a, stream);
+    if (logits_type == BITCOS_BF16) return launch_route_type<__nv_bfloat16>(a, stream);
+    return launch_route_type<__half>(a, stream);
+}
+
+size_t bitcos_group_workspace_bytes(int64_t n_pairs, int n_experts) {
+    if (n_pairs < 0 || n_pairs > INT_MAX || n_experts < 1 || n_experts > BITCOS_GROUP_EXPERTS_MAX) return 0;
+    const int blocks = sort_blocks(n_pairs);
+    return blocks == 1 ? 256 : (static_cast<size_t>(blocks) * n_experts * sizeof(int32_t) + 255) / 256 * 256;
+}
+
+int bitcos_group_pairs_slots(const int32_t *pair_expert, int64_t n_pairs, int top_k, int n_experts, int32_t *group_expert,
+                             int32_t *group_begin, int32_t *pair_xrow_sorted, int32_t *order, int32_t *slot, int32_t *n_groups,
+                             void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!pair_expert || !group_expert || !group_begin || !pair_xrow_sorted || !order || !slot || !n_groups || !workspace)
+        return BITCOS_ERR_NULL;
+    if (n_pairs < 1 || n_pairs > INT_MAX || top_k < 1 || n_experts < 1 || n_experts > BITCOS_GROUP_EXPERTS_MAX) return BITCOS_ERR_SHAPE;
+    for (const void *p : {static_cast<const void *>(pair_expert), static_cast<const void *>(group_expert), static_cast<const void *>(group_begin),
+                          static_cast<const void *>(pair_xrow_sorted), static_cast<const void *>(order), static_cast<const void *>(slot),
+                          static_cast<const void *>(n_groups), static_cast<const void *>(workspace)})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return BITCOS_ERR_ALIGN;
+    if (workspace_bytes < bitcos_group_workspace_bytes(n_pairs, n_experts)) return BITCOS_ERR_CAPACITY;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    SortArgs a{pair_expert, group_expert, group_begin, pair_xrow_sorted, order, slot, n_groups, static_cast<int32_t *>(workspace),
+               static_cast<int>(n_pairs), n_experts, top_k, 0};
+    const int blocks = sort_blocks(n_pairs);
+    a.chunk = static_cast<int>(((n_pairs + blocks - 1) / blocks + 31) / 32 * 32);
+    // threads: a warp for every 32 pairs of a chunk, but enough of them for the experts
+    int64_t threads = std::max<int64_t>((n_experts + 31) / 32 * 32, a.chunk);
+    threads = std::min<int64_t>(kSortThreads, std::max<int64_t>(threads, 128));
+    const size_t smem = (threads / 32 + 2) * static_cast<size_t>(n_experts) * sizeof(int32_t);
+    int sms = 0, budget = 0;
+    int rc = prepare_kernel<place_kernel>(&sms, &budget);
+    if (rc) return rc;
+    if (blocks > 1) {
+        rc = launch_pdl(count_kernel, dim3(static_cast<unsigned>(blocks)), kSortThreads, n_experts * sizeof(int32_t), stream, a);
+        if (rc) return rc;
+    }
+    return launch_pdl(place_kernel, dim3(static_cast<unsigned>(blocks)), static_cast<int>(threads), smem, stream, a);
+}
+
+int bitcos_combine_pairs(const void *y, int y_type, int64_t n_rows, const int32_t *slot, const float *weight, int64_t n_tokens, int top_k,
+                         int64_t M, const void *base, void *out, int out_type, void *cuda_stream) {
+    if (!y || !slot || !weight || !out) return BITCOS_ERR_NULL;
+    if (n_rows < 1 || n_tokens < 0 || n_tokens > INT_MAX || top_k < 1 || M < 1 || M > INT_MAX) return BITCOS_ERR_SHAPE;
+    if ((y_type != BITCOS_FP32 && y_type != BITCOS_BF16) || (out_type != BITCOS_FP32 && out_type != BITCOS_BF16)) return BITCOS_ERR_SHAPE;
+    if (!aligned16(y) || !aligned16(out) || (base && !aligned16(base)) || reinterpret_cast<uintptr_t>(slot) % 4 ||
+        reinterpret_cast<uintptr_t>(weight) % 4)
+        return BITCOS_ERR_ALIGN;
+    if (n_tokens == 0) return BITCOS_OK;
+    CombineArgs a{y, slot, weight, base, out, 0, M, n_rows, 0, top_k};
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (y_type == BITCOS_FP32)
+        return out_type == BITCOS_FP32 ? launch_combine<float, float>(a, n_tokens, stream) : launch_combine<float, __nv_bfloat16>(a, n_tokens, stream);
+    return out_type == BITCOS_FP32 ? launch_combine<__nv_bfloat16, float>(a, n_tokens, stream)
+                                   : launch_combine<__nv_bfloat16, __nv_bfloat16>(a, n_tokens, stream);
+}
+
+}  // extern "C"
