@@ -639,6 +639,53 @@ int bitcos_group_pairs_slots(const int32_t *pair_expert, int64_t n_pairs, int to
 int bitcos_combine_pairs(const void *y, int y_type, int64_t n_rows, const int32_t *slot, const float *weight, int64_t n_tokens, int top_k,
                          int64_t M, const void *base, void *out, int out_type, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * 8-bit floating point (e4m3) beside the ternary formats: for the matrices that a ternary checkpoint keeps in
+ * 8 bits, for prompts (any number of rows), and as the same-chip baseline at 8 bits per weight.  (The paper has no
+ * counterpart; its 16-bit group scales along K are here 32-bit scales of blocks of 128 x 128.)
+ * ------------------------------------------------------------------------------------- */
+#define BITCOS_FP8_WORKSPACE_BYTES 256
+#define BITCOS_FP8_ROWS_MAX 0x7FFFFF00
+
+/* Activations to e4m3 with one scale per row and group of 128, decided in float32:
+ *     a = max(max |x| over the group, 2^-100)     scale = a / 448     code = e4m3(x * (448 / a))
+ * (IEEE quotients and product, one rounding to nearest even; |code| <= 448; an all-zero group gets codes 0).  Values are finite.
+ *   x      device [rows][K] of x_type (BITCOS_FP32 or BITCOS_BF16), 16-byte aligned; rows 0: nothing is done
+ *   q      device bytes [rows][K] (e4m3 codes), 16-byte aligned;  scale   device float [rows][K/128] */
+int bitcos_fp8_quantize(const void *x, int x_type, int64_t rows, int64_t K, uint8_t *q, float *scale, void *cuda_stream);
+
+/* y[t][m] = sum over groups g of  x_scale[t][g] * w_scale[m/128][g] * (sum over k in g of W[m][k] * x[t][k])
+ * with e4m3 codes W and x, on the tensor cores (tcgen05): every product is exact, a group of 128 is added up in fp32 by the tensor
+ * core, the groups in fp32 in a fixed order (the bits depend on rows, M, K and the device, not on the run); rounded once to y's type.
+ *   W        device bytes [M][K], row major, 16-byte aligned;  w_scale   device float [ceil(M/128)][K/128]
+ *   x        device bytes [rows][K], 16-byte aligned;  x_scale   device float [rows][K/128], e.g. both from bitcos_fp8_quantize
+ *   rows     0 .. BITCOS_FP8_ROWS_MAX (0: nothing is done); M and K as large, K a multiple of 128
+ *   y        device [rows][M] of y_type (BITCOS_FP32 or BITCOS_BF16), 16-byte aligned, overwritten
+ *   workspace   NULL, or device scratch of BITCOS_FP8_WORKSPACE_BYTES, zero filled once (bitcos_workspace_init), whose word 0 is
+ *               the status word that bitcos_workspace_status reads (1: a bounded wait ran out, the outputs are not complete).  Nothing else is
+ *               kept in it, so calls may share one.
+ * Stream ordered like the products: W (and nothing else) may be read while an earlier kernel of this library is still running, so
+ * codes that bitcos_fp8_quantize has just written are activations, not weights, of the next call. */
+int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t K, const uint8_t *x, const float *x_scale, int64_t rows,
+                      void *y, int y_type, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* The same over the routed pairs of a mixture-of-experts layer, from the lists that bitcos_group_pairs_device or
+ * bitcos_group_pairs_slots leave on the device: pairs group_begin[i] .. group_begin[i+1]-1 use expert group_expert[i], pair p multiplies
+ * row pair_xrow[p] of x and writes y[p].  Groups may have any number of pairs.
+ *   W        device bytes [n_experts][M][K];  w_scale   device float [n_experts][ceil(M/128)][K/128]
+ *   group_expert, group_begin   device int32 [max_groups], [max_groups + 1];  n_groups_device   device int32 [1], clipped to max_groups
+ *   max_groups   1 .. BITCOS_GROUP_EXPERTS_MAX
+ *   pair_xrow   device int32 [n_pairs], or NULL: pair p reads row p (the second product of an expert)
+ *   x        device bytes [n_xrows][K];  x_scale   device float [n_xrows][K/128];  y   device [n_pairs][M]
+ * The lists are checked on the device: a group whose expert is outside [0, n_experts) or whose pairs lie outside [0, n_pairs) is
+ * skipped whole, a pair whose row is outside [0, n_xrows) alone; nothing of them is written and the status word is set
+ * to 2.  An empty group is skipped without a mark.  Rows of y that no group covers are left as they were.  W is read after every
+ * earlier kernel in the stream has completed.  Everything else as for bitcos_fp8_matmul. */
+int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_experts, int64_t M, int64_t K, const int32_t *group_expert,
+                              const int32_t *group_begin, const int32_t *n_groups_device, int max_groups, const int32_t *pair_xrow,
+                              int64_t n_pairs, const uint8_t *x, const float *x_scale, int64_t n_xrows, void *y, int y_type, void *workspace,
+                              size_t workspace_bytes, void *cuda_stream);
+
 #ifdef __GNUC__
 #pragma GCC visibility pop
 #endif

@@ -29,6 +29,7 @@ EXPORTED_SYMBOLS = [
     "bitcos_choose_format", "bitcos_count_nnz_device", "bitcos_pack_device", "bitcos_pack_device_limited", "bitcos_gemv_bf16", "bitcos_gemv_multi_bf16",
     "bitcos_gemv_multi_group_scales", "bitcos_gemv_blend_bf16", "bitcos_decode_probe_variant", "bitcos_gemv_phased", "bitcos_gemv_phases_host", "trit5_gemv_grouped", "bit2_gemv_grouped", "bitcos_gemv_static_status", "bitcos_wait_probe", "bitcos_group_pairs_device", "bitcos_gemv_grouped_lists", "bitcos_gemv_multi_chained", "bitcos_gemv_multi_plan",
     "bitcos_route_experts", "bitcos_group_workspace_bytes", "bitcos_group_pairs_slots", "bitcos_combine_pairs",
+    "bitcos_fp8_quantize", "bitcos_fp8_matmul", "bitcos_fp8_matmul_grouped",
 ]
 
 
@@ -132,6 +133,9 @@ def load_library():
     L.bitcos_group_workspace_bytes.argtypes = [i64, C.c_int]
     L.bitcos_group_pairs_slots.argtypes = [vp, i64, C.c_int, C.c_int, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.bitcos_combine_pairs.argtypes = [vp, C.c_int, i64, vp, vp, i64, C.c_int, i64, vp, vp, C.c_int, vp]
+    L.bitcos_fp8_quantize.argtypes = [vp, C.c_int, i64, i64, vp, vp, vp]
+    L.bitcos_fp8_matmul.argtypes = [vp, vp, i64, i64, vp, vp, i64, vp, C.c_int, vp, sz, vp]
+    L.bitcos_fp8_matmul_grouped.argtypes = [vp, vp, C.c_int, i64, i64, vp, vp, vp, C.c_int, vp, i64, vp, vp, i64, vp, C.c_int, vp, sz, vp]
     _bind_calls(L)
     _lib = L
     return L
@@ -994,3 +998,108 @@ def bitcos_combine_pairs(y, slot, weight, base=None, out=None, out_dtype=None):
     if status:
         _check(status, "bitcos_combine_pairs")
     return out
+
+
+# ---------------------------------------------------------------------------------------------
+# 8-bit floating point
+# ---------------------------------------------------------------------------------------------
+FP8_WORKSPACE_BYTES = 256
+
+
+class Fp8Weights:
+    """e4m3 weights with one float32 scale per block of 128 x 128: codes [M, K] with scales [ceil(M / 128), K / 128], or the
+    experts of a layer, codes [experts, M, K] with scales [experts, ceil(M / 128), K / 128]."""
+
+    def __init__(self, codes, scales):
+        import torch
+        _require(codes.dtype == torch.float8_e4m3fn and codes.dim() in (2, 3) and codes.is_contiguous(),
+                 "codes must be a contiguous float8_e4m3fn [M, K] or [experts, M, K] tensor")
+        M, K = codes.shape[-2:]
+        _require(K % GROUP == 0 and K > 0, "K must be a multiple of 128")
+        _require(scales.dtype == torch.float32 and scales.is_contiguous() and scales.get_device() == codes.get_device() and
+                 scales.shape == (*codes.shape[:-2], (M + GROUP - 1) // GROUP, K // GROUP),
+                 "scales must be a contiguous float32 [(experts,) ceil(M / 128), K / 128] tensor on the codes' device")
+        self.codes, self.scales, self.M, self.K = codes, scales, M, K
+        self.experts = codes.shape[0] if codes.dim() == 3 else None
+
+    def payload_bytes(self) -> int:
+        return self.codes.numel() + self.scales.numel() * 4
+
+
+def make_fp8_workspace(device="cuda"):
+    """Zero-filled device scratch for the e4m3 products: their status word (workspace_status)."""
+    import torch
+    return torch.zeros(FP8_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+
+
+def bitcos_fp8_quantize(x, q=None, scale=None):
+    """Activations [rows, K] (float32 or bfloat16) -> (e4m3 codes [rows, K], float32 scales [rows, K / 128])."""
+    import torch
+    _require(x.dim() == 2 and x.is_contiguous(), "x must be a contiguous [rows, K] tensor")
+    rows, K = x.shape
+    code = _type_code(x.dtype, (0, 1), "x")
+    if q is None:
+        q = torch.empty((rows, K), dtype=torch.float8_e4m3fn, device=x.device)
+    if scale is None:
+        scale = torch.empty((rows, K // GROUP), dtype=torch.float32, device=x.device)
+    _require(q.dtype == torch.float8_e4m3fn and q.shape == x.shape and q.is_contiguous(), "q must be a contiguous float8_e4m3fn tensor shaped as x")
+    _require(scale.dtype == torch.float32 and scale.shape == (rows, K // GROUP) and scale.is_contiguous(), "scale must be contiguous float32 [rows, K / 128]")
+    stream = _stream_of(x, q, scale)
+    status = (_calls or _native()).bitcos_fp8_quantize(x.data_ptr(), code, rows, K, q.data_ptr(), scale.data_ptr(), stream) if rows else 0
+    if status:
+        _check(status, "bitcos_fp8_quantize")
+    return q, scale
+
+
+def _fp8_operands(W, x, x_scale, rows_out, y, out_dtype, workspace):
+    """Checks what both products take; returns (y, its type's number)."""
+    import torch
+    _require(x.dtype == torch.float8_e4m3fn and x.dim() == 2 and x.shape[1] == W.K and x.is_contiguous(), "x must be a contiguous float8_e4m3fn [rows, K] tensor")
+    _require(x_scale.dtype == torch.float32 and x_scale.shape == (x.shape[0], W.K // GROUP) and x_scale.is_contiguous(),
+             "x_scale must be a contiguous float32 [rows, K / 128] tensor")
+    if y is None:
+        y = torch.empty((rows_out, W.M), dtype=out_dtype or torch.float32, device=x.device)
+    _require(y.shape == (rows_out, W.M) and y.is_contiguous() and (out_dtype is None or y.dtype == out_dtype), "y must be a contiguous [rows, M] tensor")
+    return y, _type_code(y.dtype, (0, 1), "y")
+
+
+def bitcos_fp8_matmul(W: Fp8Weights, x, x_scale, y=None, out_dtype=None, workspace=None):
+    """x [rows, K] (e4m3, scales [rows, K / 128]) times the rows of W: y [rows, M], float32 (default) or bfloat16."""
+    _require(W.experts is None, "W holds experts: use bitcos_fp8_matmul_grouped")
+    rows = x.shape[0]
+    y, code = _fp8_operands(W, x, x_scale, rows, y, out_dtype, workspace)
+    stream = _stream_of(W.codes, x, x_scale, y, workspace)
+    status = (_calls or _native()).bitcos_fp8_matmul(
+        W.codes.data_ptr(), W.scales.data_ptr(), W.M, W.K, x.data_ptr(), x_scale.data_ptr(), rows, y.data_ptr(), code,
+        0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+        stream) if rows else 0
+    if status:
+        _check(status, "bitcos_fp8_matmul")
+    return y
+
+
+def bitcos_fp8_matmul_grouped(W: Fp8Weights, group_expert, group_begin, n_groups, pair_xrow, x, x_scale, y=None, out_dtype=None,
+                              workspace=None, n_pairs=None):
+    """The product over routed pairs grouped by expert (device int32 lists, as bitcos_group_pairs_device and
+    bitcos_group_pairs_slots return them): pair p multiplies row pair_xrow[p] of x (pair_xrow None: row p, n_pairs of them) with its
+    group's expert and writes y[p]; rows of y that no group covers are left as they were."""
+    import torch
+    _require(W.experts is not None, "W must hold experts ([experts, M, K])")
+    for t in (group_expert, group_begin, n_groups, pair_xrow):
+        _require(t is None or (t.dtype == torch.int32 and t.is_contiguous()), "the lists must be contiguous int32 tensors")
+    if pair_xrow is not None:
+        n_pairs = pair_xrow.numel()
+    elif n_pairs is None:
+        n_pairs = x.shape[0]
+    max_groups = group_expert.numel()
+    _require(group_begin.numel() > max_groups and n_groups.numel() >= 1, "group_begin must have one entry more than group_expert")
+    y, code = _fp8_operands(W, x, x_scale, n_pairs, y, out_dtype, workspace)
+    stream = _stream_of(W.codes, group_expert, group_begin, n_groups, pair_xrow, x, x_scale, y, workspace)
+    status = (_calls or _native()).bitcos_fp8_matmul_grouped(
+        W.codes.data_ptr(), W.scales.data_ptr(), W.experts, W.M, W.K, group_expert.data_ptr(), group_begin.data_ptr(), n_groups.data_ptr(),
+        max_groups, 0 if pair_xrow is None else pair_xrow.data_ptr(), n_pairs, x.data_ptr(), x_scale.data_ptr(), x.shape[0], y.data_ptr(), code,
+        0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+        stream) if n_pairs else 0
+    if status:
+        _check(status, "bitcos_fp8_matmul_grouped")
+    return y

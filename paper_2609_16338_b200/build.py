@@ -17,6 +17,7 @@ CALLS_SOURCE = os.path.join(CSRC, "calls.c")
 INST = os.path.join(CSRC, "gemv_inst.cu")
 INST_PARTS = 11             # the parts of gemv_inst.cuh, each compiled by a process of its own
 SOURCES = [os.path.join(CSRC, "gemv.cu"), os.path.join(CSRC, "probe.cu"), os.path.join(CSRC, "pack_device.cu"), os.path.join(CSRC, "route.cu"),
+           os.path.join(CSRC, "fp8.cu"),
            os.path.join(CSRC, "pack.cpp")]
 HEADERS = [INST, *(os.path.join(CSRC, h) for h in ("gemv.cuh", "gemv_inst.cuh", "decode.cuh", "common.cuh")),
            os.path.join(ROOT, "include", "bitcos.h")]

@@ -108,13 +108,24 @@ CALL(bitcos_group_pairs_slots, 13,
 /* (y, y_type, n_rows, slot, weight, n_tokens, top_k, M, base, out, out_type, stream) */
 CALL(bitcos_combine_pairs, 12, TYPES(void *, int, int64_t, void *, void *, int64_t, int, int64_t, void *, void *, int, void *), P(0),
      I(1), L(2), P(3), P(4), L(5), I(6), L(7), P(8), P(9), I(10), P(11))
+/* (x, x_type, rows, K, q, scale, stream) */
+CALL(bitcos_fp8_quantize, 7, TYPES(void *, int, int64_t, int64_t, void *, void *, void *), P(0), I(1), L(2), L(3), P(4), P(5), P(6))
+/* (W, w_scale, M, K, x, x_scale, rows, y, y_type, workspace, workspace_bytes, stream) */
+CALL(bitcos_fp8_matmul, 12, TYPES(void *, void *, int64_t, int64_t, void *, void *, int64_t, void *, int, void *, size_t, void *), P(0),
+     P(1), L(2), L(3), P(4), P(5), L(6), P(7), I(8), P(9), Z(10), P(11))
+/* (W, w_scale, n_experts, M, K, group_expert, group_begin, n_groups, max_groups, pair_xrow, n_pairs, x, x_scale, n_xrows, y, y_type,
+   workspace, workspace_bytes, stream) */
+CALL(bitcos_fp8_matmul_grouped, 19,
+     TYPES(void *, void *, int, int64_t, int64_t, void *, void *, void *, int, void *, int64_t, void *, void *, int64_t, void *, int, void *,
+           size_t, void *),
+     P(0), P(1), I(2), L(3), L(4), P(5), P(6), P(7), I(8), P(9), L(10), P(11), P(12), L(13), P(14), I(15), P(16), Z(17), P(18))
 
 #define EVERY(X)                                                                                                           \
     X(bitcos_gemv) X(bitcos_gemv_group_scales) X(bitcos_gemv_bf16) X(bitcos_gemv_blend_bf16) X(trit5_gemv) X(bit2_gemv)    \
     X(bitcos_gemv_multi) X(bitcos_gemv_multi_bf16) X(bitcos_gemv_multi_group_scales) X(bitcos_gemv_multi_chained)          \
     X(bitcos_gemv_phases_host) X(bitcos_quantize_activations) X(bitcos_group_pairs_device) X(bitcos_gemv_grouped)          \
     X(trit5_gemv_grouped) X(bit2_gemv_grouped) X(bitcos_gemv_grouped_lists) X(bitcos_route_experts)                           \
-    X(bitcos_group_pairs_slots) X(bitcos_combine_pairs)
+    X(bitcos_group_pairs_slots) X(bitcos_combine_pairs) X(bitcos_fp8_quantize) X(bitcos_fp8_matmul) X(bitcos_fp8_matmul_grouped)
 
 /* bind(name, address): where the library's function is */
 static PyObject *bind(PyObject *self, PyObject *args) {

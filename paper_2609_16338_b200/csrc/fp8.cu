@@ -1,0 +1,838 @@
+// 8-bit floating point beside the packed ternary formats: the quantiser to e4m3 with one scale per row and group of 128,
+// and the product of e4m3 activations with e4m3 weights that carry one scale per block of 128 x 128,
+//
+//     y[t][m] = sum over groups g of  xs[t][g] * ws[m / 128][g] * (sum over k in g of W[m][k] * x[t][k]),
+//
+// dense and over the routed pairs of a mixture-of-experts layer.
+//
+// The scales change with every group of 128, so the tensor cores may add up one group only: each group is four
+// tcgen05.mma (K = 32) into a fresh accumulator in tensor memory, and warps of their own ("promoters") read it back, multiply with
+// the two scales and add in fp32 registers while the next group is being multiplied into the other accumulator.
+//
+// Two operand orders, chosen by the host (choose_dense, choose_grouped):
+//   tokens first   A = 128 tokens, B = 256 weight rows.  A promoter thread holds one token's 128 columns; the scales of a group are
+//                  one number per thread.  Tiles are spread over persistent blocks.  For prompts.
+//   weights first  A = 128 weight rows, B = 16 .. 128 tokens.  The weights pass once for up to 128 tokens, two blocks per
+//                  multiprocessor keep enough of them in flight, and K is cut over the blocks of a cluster where there are few row
+//                  blocks: each leaves its sums in shared memory, and the cluster adds them in order of rank (no workspace, no
+//                  atomics, the same bits every time).  For decoding.
+//
+// Operands come by TMA (128-byte swizzle, 128 bytes of K per stage); the rows of routed pairs by tile::gather4.
+#include "bitcos.h"
+#include "common.cuh"
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <climits>
+
+using namespace bitcos_kernels;
+
+namespace {
+
+constexpr int kGroup = BITCOS_GROUP;
+constexpr uint32_t kFull = 0xFFFFFFFFu;
+constexpr float kE4m3Max = 448.0f;
+
+// ------------------------------------------------------------------ quantiser
+//     a = max(max |x| over the group, 2^-100),  scale = a / 448,  code = e4m3(x * (448 / a))
+// IEEE quotients and product, one rounding to nearest even.  Sixteen lanes per group of 128, eight values a lane.
+// Bound by memory.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p) {
+        a = __ldg(reinterpret_cast<const float4 *>(p));
+        b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+};
+template <>
+struct Eight<__nv_bfloat16> {
+    uint4 a;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = __ldg(reinterpret_cast<const uint4 *>(p)); }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        v[0] = bf16_lo(a.x), v[1] = bf16_hi(a.x), v[2] = bf16_lo(a.y), v[3] = bf16_hi(a.y);
+        v[4] = bf16_lo(a.z), v[5] = bf16_hi(a.z), v[6] = bf16_lo(a.w), v[7] = bf16_hi(a.w);
+    }
+};
+
+__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+constexpr int kQuantGroups = 4;           // groups per half warp, so that as many loads are under way
+template <typename T>
+__global__ void __launch_bounds__(256) fp8_quantize_kernel(const T *__restrict__ x, uint8_t *__restrict__ q, float *__restrict__ scale,
+                                                           int64_t n_groups) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int part = threadIdx.x & 15, half = threadIdx.x >> 4;
+    const int64_t first = (static_cast<int64_t>(blockIdx.x) * kQuantGroups * 16) + half;
+    Eight<T> in[kQuantGroups];
+#pragma unroll
+    for (int i = 0; i < kQuantGroups; ++i)
+        if (first + i * 16 < n_groups) in[i].load(x + (first + i * 16) * kGroup + part * 8);
+#pragma unroll
+    for (int i = 0; i < kQuantGroups; ++i) {
+        const int64_t grp = first + i * 16;
+        if (grp >= n_groups) break;                 // (the same for all sixteen lanes; the shuffles name only those)
+        float v[8];
+        in[i].get(v);
+        float a = fabsf(v[0]);
+#pragma unroll
+        for (int j = 1; j < 8; ++j) a = fmaxf(a, fabsf(v[j]));
+        const uint32_t lanes = 0xFFFFu << (threadIdx.x & 16);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) a = fmaxf(a, __shfl_xor_sync(lanes, a, d));
+        a = fmaxf(a, kAmaxFloor);
+        const float factor = __fdiv_rn(kE4m3Max, a);
+        uint2 code;
+        code.x = e4m3_pair(__fmul_rn(v[0], factor), __fmul_rn(v[1], factor)) | (e4m3_pair(__fmul_rn(v[2], factor), __fmul_rn(v[3], factor)) << 16);
+        code.y = e4m3_pair(__fmul_rn(v[4], factor), __fmul_rn(v[5], factor)) | (e4m3_pair(__fmul_rn(v[6], factor), __fmul_rn(v[7], factor)) << 16);
+        *reinterpret_cast<uint2 *>(q + grp * kGroup + part * 8) = code;
+        if (part == 0) scale[grp] = __fdiv_rn(a, kE4m3Max);
+    }
+}
+
+// ------------------------------------------------------------------ product: device side
+constexpr int kARows = 128;               // rows of the A operand
+constexpr uint32_t kABytes = kARows * kGroup;
+constexpr int kMaxGroups = BITCOS_GROUP_EXPERTS_MAX;
+constexpr int kMaxSplits = 8;             // portable cluster size
+
+struct Fp8Args {
+    const float *w_scale;       // [experts][w_blocks][G]
+    const float *x_scale;       // [x rows][G]
+    void *y;
+    unsigned int *status;       // NULL, or the workspace's status word
+    int64_t M;
+    int64_t rows;               // dense: tokens; grouped: pairs
+    int G;                      // groups of 128 along K
+    int w_blocks;               // ceil(M / 128)
+    int out_bf16;
+    int vector;                 // rows of y may be written 16 bytes at a time
+    int splits;                 // blocks of a cluster, each with its share of K (weights first, dense)
+    int row_tiles, w_tiles;     // dense: tiles along the tokens, along the weights (grouped: w_tiles only)
+    // grouped
+    const int32_t *group_expert, *group_begin, *n_groups, *pair_xrow;
+    int max_groups, n_experts, n_xrows;
+};
+
+struct Tile {
+    int64_t row0;               // first token / pair
+    int rows;                   // tokens / pairs of the tile
+    int w0;                     // first weight row
+    int expert;
+};
+
+template <int N, bool TOK, bool GROUPED>
+struct Layout {
+    static constexpr uint32_t kBBytes = N * kGroup;
+    static constexpr uint32_t kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = TOK ? 4 : N <= 32 ? 5 : N == 64 ? 4 : 3;
+    static constexpr int kPromoters = TOK ? 8 : 4;      // warps
+    static constexpr int kThreads = 64 + kPromoters * 32;
+    static constexpr int kRowsPerTile = TOK ? kARows : N;
+    static constexpr int kWRowsPerTile = TOK ? N : kARows;
+    static constexpr uint32_t kColumns = 2 * N < 32 ? 32 : 2 * N;
+    // byte offsets behind the stages
+    static constexpr uint32_t kBars = kStages * kStageBytes;
+    static constexpr uint32_t kTmem = kBars + (2 * kStages + 4) * 8;
+    static constexpr uint32_t kScales = (kTmem + 16 + 15) / 16 * 16;
+    static constexpr uint32_t kPrefix = kScales + (TOK ? 0 : kPromoters * 2 * N * 4);
+    static constexpr uint32_t kTotal = kPrefix + (GROUPED ? (kMaxGroups + 1) * 8 : 0);
+    static constexpr uint32_t kDynamic = kTotal + 1024;  // (the stages start on a 1024-byte boundary)
+};
+
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+                 "r"(c0), "r"(c1), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int c0, const int (&r)[4], uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+        "l"(map), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(bar)
+        : "memory");
+}
+
+// Shared-memory matrix descriptor: K-major rows of 128 bytes, 128-byte swizzle, eight rows (1024 bytes) apart per step.
+__device__ __forceinline__ uint64_t matrix_desc(uint32_t addr) {
+    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptor: e4m3 x e4m3 -> fp32, M = 128, N as given.
+__host__ __device__ constexpr uint32_t instruction_desc(int n) {
+    return (1u << 4) | (static_cast<uint32_t>(n / 8) << 17) | (static_cast<uint32_t>(kARows / 16) << 24);
+}
+__device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+}
+// (the registers pass through, so that nothing that reads them is moved in front of the wait)
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
+// A bounded wait by a whole warp, which goes on or gives up as one (what follows are instructions of whole warps).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(kFull, mbar_wait(bar, parity)); }
+// a += d * s, two at a time
+__device__ __forceinline__ void fma_pair(float &a0, float &a1, uint32_t d0, uint32_t d1, float s0, float s1) {
+    asm("{\n\t.reg .b64 a, d, s;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 d, {%2, %3};\n\tmov.b64 s, {%4, %5};\n\t"
+        "fma.rn.f32x2 a, d, s, a;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "+f"(a0), "+f"(a1)
+        : "r"(d0), "r"(d1), "f"(s0), "f"(s1));
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ float cluster_load(uint32_t addr, uint32_t rank) {
+    float v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(addr), "r"(rank) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+
+// Where tile t lies.  Dense: bands of 16 tiles along the tokens, inside a band the tokens vary fastest, so that the tiles
+// that run at the same time share rows and weights in L2.  Grouped: the group by bisection in the running tile counts; inside a group
+// the tokens vary fastest (the tiles of one stretch of weights run side by side).
+template <int N, bool TOK, bool GROUPED>
+__device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefix, int n_groups, int64_t t) {
+    using L = Layout<N, TOK, GROUPED>;
+    Tile r;
+    if constexpr (!GROUPED) {
+        constexpr int kBand = 16;
+        const int64_t per_band = static_cast<int64_t>(kBand) * a.w_tiles;
+        const int band = static_cast<int>(t / per_band);
+        const int wide = min(kBand, a.row_tiles - band * kBand);
+        const int in = static_cast<int>(t - band * per_band);
+        const int w = in / wide, row_tile = band * kBand + in - w * wide;
+        r.row0 = static_cast<int64_t>(row_tile) * L::kRowsPerTile;
+        r.rows = static_cast<int>(min(static_cast<int64_t>(L::kRowsPerTile), a.rows - r.row0));
+        r.w0 = w * L::kWRowsPerTile;
+        r.expert = 0;
+    } else {
+        int lo = 0, hi = n_groups;                 // prefix[lo] <= t < prefix[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (prefix[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        const int begin = __ldg(a.group_begin + lo), end = __ldg(a.group_begin + lo + 1);
+        const int row_tiles = (end - begin + L::kRowsPerTile - 1) / L::kRowsPerTile;
+        const int in = static_cast<int>(t - prefix[lo]);
+        const int w = in / row_tiles, row_tile = in - w * row_tiles;
+        r.row0 = begin + static_cast<int64_t>(row_tile) * L::kRowsPerTile;
+        r.rows = min(L::kRowsPerTile, static_cast<int>(end - r.row0));
+        r.w0 = w * L::kWRowsPerTile;
+        r.expert = __ldg(a.group_expert + lo);
+    }
+    return r;
+}
+
+template <int N, bool TOK, bool GROUPED>
+__global__ void __launch_bounds__(Layout<N, TOK, GROUPED>::kThreads, TOK ? 1 : 2)
+fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ Fp8Args a) {
+    using L = Layout<N, TOK, GROUPED>;
+    constexpr int kStages = L::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_addr(smem_raw);
+    uint8_t *smem = smem_raw + (1024u - (raw & 1023u)) % 1024u;
+    const uint32_t base = smem_addr(smem);
+    const uint32_t full = base + L::kBars, empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
+    int64_t *prefix = reinterpret_cast<int64_t *>(smem + L::kPrefix);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int splits = GROUPED || TOK ? 1 : a.splits;
+    const int rank = splits > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const int k0 = static_cast<int>(static_cast<int64_t>(a.G) * rank / splits), k1 = static_cast<int>(static_cast<int64_t>(a.G) * (rank + 1) / splits);
+
+    if (warp == 0 && lane == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full + 8 * b, 1);
+            mbar_init(acc_empty + 8 * b, L::kPromoters);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if constexpr (!GROUPED) {
+            // the first weights are on their way before the kernel in front of this one has finished: they are nobody's output
+            if (blockIdx.x / splits < static_cast<int64_t>(a.row_tiles) * a.w_tiles) {
+                const Tile t = find_tile<N, TOK, GROUPED>(a, prefix, 0, blockIdx.x / splits);
+                for (int i = 0; i < kStages && k0 + i < k1; ++i) {
+                    const uint32_t dst = base + i * L::kStageBytes + (TOK ? kABytes : 0);
+                    mbar_expect_tx(full + 8 * i, L::kStageBytes);
+                    tma_3d(dst, &wmap, (k0 + i) * kGroup, t.w0, 0, full + 8 * i);
+                }
+            }
+        }
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kTmem), "n"(L::kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        tmem_fence_before();
+    }
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + L::kTmem);
+    // The next kernel's blocks may start only once every block of this one holds its tensor memory: a block of the next kernel that
+    // got it first would keep it until this kernel is done.
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    int n_groups = 0;
+    int64_t n_tiles = static_cast<int64_t>(a.row_tiles) * a.w_tiles;
+    if constexpr (GROUPED) {
+        n_groups = min(max(__ldg(a.n_groups), 0), a.max_groups);
+        if (warp == 0) {
+            int64_t sum = 0;
+            for (int g0 = 0; g0 < n_groups; g0 += 32) {
+                const int g = g0 + lane;
+                int64_t tiles = 0;
+                if (g < n_groups) {
+                    const int e = __ldg(a.group_expert + g), begin = __ldg(a.group_begin + g), end = __ldg(a.group_begin + g + 1);
+                    if (end > begin) {
+                        // a malformed group is skipped whole and marked (an empty one without a mark)
+                        if (e >= 0 && e < a.n_experts && begin >= 0 && end <= a.rows)
+                            tiles = static_cast<int64_t>((end - begin + L::kRowsPerTile - 1) / L::kRowsPerTile) * a.w_tiles;
+                        else if (a.status && blockIdx.x == 0) *a.status = 2u;
+                    }
+                }
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int64_t up = __shfl_up_sync(kFull, tiles, d);
+                    if (lane >= d) tiles += up;
+                }
+                if (g < n_groups) prefix[g + 1] = sum + tiles;
+                sum += __shfl_sync(kFull, tiles, 31);
+            }
+            if (lane == 0) prefix[0] = 0;
+        }
+        __syncthreads();
+        n_tiles = prefix[n_groups];
+    }
+    const int64_t t_first = blockIdx.x / splits, t_step = gridDim.x / splits;
+    bool ok = true;
+    uint32_t it = 0;                       // groups of 128 so far, over all tiles
+
+    if (warp == 0) {
+        // ---- producer
+        for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
+            const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
+            int src[4] = {0, 0, 0, 0};
+            if constexpr (GROUPED) {
+                // rows 4 lane .. + 3 of the tile; what is not a row of the tile, or no row of x, reads some row of x and is dropped later
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = lane * 4 + j;
+                    const int r = i < tile.rows ? (a.pair_xrow ? __ldg(a.pair_xrow + tile.row0 + i) : static_cast<int>(tile.row0 + i)) : 0;
+                    src[j] = r >= 0 && r < a.n_xrows ? r : 0;
+                }
+            }
+            for (int kb = k0; ok && kb < k1; ++kb, ++it) {
+                const uint32_t s = it % kStages;
+                const uint32_t stage = base + s * L::kStageBytes, bar = full + 8 * s;
+                const uint32_t w_dst = stage + (TOK ? kABytes : 0), x_dst = stage + (TOK ? 0 : kABytes);
+                if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
+                    ok = false;
+                    break;
+                }
+                const bool sent = !GROUPED && it < kStages && t == t_first;       // (announced and the weights sent above)
+                if (lane == 0 && !sent) {
+                    mbar_expect_tx(bar, L::kStageBytes);
+                    tma_3d(w_dst, &wmap, kb * kGroup, tile.w0, tile.expert, bar);
+                }
+                if constexpr (GROUPED) {
+                    __syncwarp();
+                    if (lane < L::kRowsPerTile / 4) tma_gather4(x_dst + lane * 512, &xmap, kb * kGroup, src, bar);
+                } else if (lane == 0) {
+                    tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), bar);
+                }
+            }
+        }
+        // no copy may outlive the block
+        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) ok &= mbar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
+    } else if (warp == 1) {
+        // ---- tensor cores: one lane
+        if (lane == 0) {
+            constexpr uint32_t idesc = instruction_desc(N);
+            for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
+                for (int kb = k0; kb < k1; ++kb, ++it) {
+                    const uint32_t s = it % kStages, b = it & 1;
+                    if (it >= 2 && !mbar_wait(acc_empty + 8 * b, (it / 2 - 1) & 1)) {
+                        ok = false;
+                        break;
+                    }
+                    if (!mbar_wait(full + 8 * s, (it / kStages) & 1)) {
+                        ok = false;
+                        break;
+                    }
+                    tmem_fence_after();
+                    const uint64_t da = matrix_desc(base + s * L::kStageBytes), db = matrix_desc(base + s * L::kStageBytes + kABytes);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_e4m3(tmem + b * N, da + 2 * k, db + 2 * k, idesc, k > 0);
+                    mma_commit(empty + 8 * s);
+                    mma_commit(acc_full + 8 * b);
+                }
+            }
+            // nothing may be in flight when the tensor memory goes
+            for (uint32_t i = it > 2 ? it - 2 : 0; i < it; ++i) ok &= mbar_wait(acc_full + 8 * (i & 1), (i / 2) & 1);
+        }
+        __syncwarp();
+    } else {
+        // ---- promoters: warp w of four reads lanes 32 (w % 4) .. + 31 of the accumulators
+        const int quarter = warp & 3, half = TOK ? (warp - 2) >> 2 : 0;
+        const int row = quarter * 32 + lane;       // of A
+        const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + half * 128;
+        constexpr int kCols = TOK ? 128 : N;
+        for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
+            const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
+            float acc[kCols];
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
+            const float *ws = a.w_scale + (static_cast<int64_t>(tile.expert) * a.w_blocks) * a.G;
+            if constexpr (TOK) {
+                const int block = tile.w0 / kGroup + half;
+                const bool columns = block < a.w_blocks;
+                ws += static_cast<int64_t>(columns ? block : 0) * a.G;
+                bool mine = row < tile.rows;
+                int64_t xr = tile.row0 + row;
+                if (GROUPED && a.pair_xrow && mine) xr = __ldg(a.pair_xrow + xr);
+                if (GROUPED && mine && (xr < 0 || xr >= a.n_xrows)) {
+                    mine = false;
+                    if (a.status) *a.status = 2u;
+                }
+                const float *xs = a.x_scale + (mine ? xr : 0) * a.G;
+                float sx = __ldg(xs + k0), sw = __ldg(ws + k0);
+                for (int kb = k0; kb < k1; ++kb, ++it) {
+                    const uint32_t b = it & 1;
+                    const float s = sx * sw;
+                    if (kb + 1 < k1) {
+                        sx = __ldg(xs + kb + 1);
+                        sw = __ldg(ws + kb + 1);
+                    }
+                    if (!warp_wait(acc_full + 8 * b, (it / 2) & 1)) {
+                        ok = false;
+                        break;
+                    }
+                    tmem_fence_after();
+                    uint32_t d[2][16];
+                    tmem_load16(tmem_row + b * N, d[0]);
+                    tmem_wait16(d[0]);
+#pragma unroll
+                    for (int c = 0; c < kCols / 16; ++c) {
+                        if (c + 1 < kCols / 16) tmem_load16(tmem_row + b * N + (c + 1) * 16, d[(c + 1) & 1]);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) fma_pair(acc[c * 16 + i], acc[c * 16 + i + 1], d[c & 1][i], d[c & 1][i + 1], s, s);
+                        if (c + 1 < kCols / 16) tmem_wait16(d[(c + 1) & 1]);
+                        if (c + 2 == kCols / 16) {
+                            tmem_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(acc_empty + 8 * b);
+                        }
+                    }
+                }
+                if (!ok) break;
+                const int64_t c0 = tile.w0 + half * 128;
+                if (mine && columns) {
+                    const int valid = static_cast<int>(min(static_cast<int64_t>(128), a.M - c0));
+                    const int64_t at = (tile.row0 + row) * a.M + c0;
+                    if (a.out_bf16) {
+                        __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.y) + at;
+#pragma unroll
+                        for (int i = 0; i < 128; i += 8) {
+                            if (a.vector && i + 8 <= valid) {
+                                *reinterpret_cast<uint4 *>(out + i) = make_uint4(bf16_pair(acc[i], acc[i + 1]), bf16_pair(acc[i + 2], acc[i + 3]),
+                                                                                 bf16_pair(acc[i + 4], acc[i + 5]), bf16_pair(acc[i + 6], acc[i + 7]));
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    if (i + j < valid) out[i + j] = __float2bfloat16_rn(acc[i + j]);
+                            }
+                        }
+                    } else {
+                        float *out = static_cast<float *>(a.y) + at;
+#pragma unroll
+                        for (int i = 0; i < 128; i += 4) {
+                            if (a.vector && i + 4 <= valid) {
+                                *reinterpret_cast<float4 *>(out + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    if (i + j < valid) out[i + j] = acc[i + j];
+                            }
+                        }
+                    }
+                }
+            } else {
+                ws += static_cast<int64_t>(tile.w0 / kGroup) * a.G;
+                // the scales of the tile's tokens: lane l looks after columns l, l + 32, ...; a group's products with the weights'
+                // scale pass through shared memory, a copy per warp
+                constexpr int kOwn = (N + 31) / 32;
+                float *scales = reinterpret_cast<float *>(smem + L::kScales) + (warp - 2) * 2 * N;
+                const float *xs[kOwn];
+                uint32_t bad[kOwn];                // columns whose row of x does not exist: not written
+                float sx[kOwn];
+                float sw = __ldg(ws + k0);
+#pragma unroll
+                for (int j = 0; j < kOwn; ++j) {
+                    const int n = lane + 32 * j;
+                    bool there = n < tile.rows;
+                    int64_t xr = tile.row0 + n;
+                    if (GROUPED && a.pair_xrow && there) xr = __ldg(a.pair_xrow + xr);
+                    const bool wrong = GROUPED && there && (xr < 0 || xr >= a.n_xrows);
+                    bad[j] = __ballot_sync(kFull, wrong);
+                    if (wrong) {
+                        there = false;
+                        if (a.status) *a.status = 2u;
+                    }
+                    xs[j] = there ? a.x_scale + xr * a.G : nullptr;
+                    sx[j] = there ? __ldg(xs[j] + k0) : 0.f;
+                }
+                for (int kb = k0; kb < k1; ++kb, ++it) {
+                    const uint32_t b = it & 1;
+                    float *scale = scales + b * N;
+#pragma unroll
+                    for (int j = 0; j < kOwn; ++j) {
+                        if (N % 32 == 0 || lane < N) scale[lane + 32 * j] = sx[j] * sw;
+                        if (kb + 1 < k1 && xs[j]) sx[j] = __ldg(xs[j] + kb + 1);
+                    }
+                    if (kb + 1 < k1) sw = __ldg(ws + kb + 1);
+                    __syncwarp();
+                    if (!warp_wait(acc_full + 8 * b, (it / 2) & 1)) {
+                        ok = false;
+                        break;
+                    }
+                    tmem_fence_after();
+                    uint32_t d[2][16];
+                    tmem_load16(tmem_row + b * N, d[0]);
+                    tmem_wait16(d[0]);
+#pragma unroll
+                    for (int c = 0; c < kCols / 16; ++c) {
+                        if (c + 1 < kCols / 16) tmem_load16(tmem_row + b * N + (c + 1) * 16, d[(c + 1) & 1]);
+                        if (kCols == 16 || c + 1 == kCols / 16) {
+                            tmem_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(acc_empty + 8 * b);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            const float4 sc = *reinterpret_cast<const float4 *>(scale + c * 16 + i);
+                            fma_pair(acc[c * 16 + i], acc[c * 16 + i + 1], d[c & 1][i], d[c & 1][i + 1], sc.x, sc.y);
+                            fma_pair(acc[c * 16 + i + 2], acc[c * 16 + i + 3], d[c & 1][i + 2], d[c & 1][i + 3], sc.z, sc.w);
+                        }
+                        if (c + 1 < kCols / 16) tmem_wait16(d[(c + 1) & 1]);
+                    }
+                }
+                if (!ok) break;
+                const int64_t m = tile.w0 + row;
+                if (splits == 1) {
+                    if (m < a.M) {
+#pragma unroll
+                        for (int n = 0; n < N; ++n) {
+                            if (n < tile.rows && !((bad[n / 32] >> (n % 32)) & 1u)) {
+                                const int64_t at = (tile.row0 + n) * a.M + m;
+                                if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.y)[at] = __float2bfloat16_rn(acc[n]);
+                                else static_cast<float *>(a.y)[at] = acc[n];
+                            }
+                        }
+                    }
+                } else {
+                    // (every stage has been read: the last group's accumulator is complete)
+                    float *sums = reinterpret_cast<float *>(smem);
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        if (n < tile.rows) sums[n * kARows + row] = acc[n];
+                }
+            }
+        }
+    }
+    if (!ok && a.status) *a.status = 1u;
+
+    if constexpr (!GROUPED && !TOK) {
+        if (splits > 1) {
+            cluster_sync();
+            if (warp >= 2) {
+                const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t_first);
+                const int row = (warp & 3) * 32 + lane;
+                const int64_t m = tile.w0 + row;
+                for (int n = rank; n < tile.rows; n += splits) {
+                    float sum = 0.f;
+                    for (int r = 0; r < splits; ++r) sum += cluster_load(base + static_cast<uint32_t>(n * kARows + row) * 4u, r);
+                    const int64_t at = (tile.row0 + n) * a.M + m;
+                    if (m < a.M) {
+                        if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.y)[at] = __float2bfloat16_rn(sum);
+                        else static_cast<float *>(a.y)[at] = sum;
+                    }
+                }
+            }
+            cluster_sync();                // (nobody's sums go while they may be read)
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tmem_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kColumns) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------ product: host side
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
+}
+
+// Rows of K bytes, box_rows of them and 128 bytes of each per copy; experts > 0: a third dimension of that many matrices.
+int encode(CUtensorMap *map, const void *data, int64_t K, int64_t rows, int experts, int box_rows) {
+    const EncodeTiled f = encode_tiled();
+    if (!f) {
+        g_last_cuda_error = cudaErrorNotSupported;
+        return BITCOS_ERR_CUDA;
+    }
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(experts > 0 ? experts : 1)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(K) * static_cast<cuuint64_t>(rows)};
+    const cuuint32_t box[3] = {kGroup, static_cast<cuuint32_t>(box_rows), 1}, ones[3] = {1, 1, 1};
+    const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, experts > 0 ? 3 : 2, const_cast<void *>(data), dims, strides, box, ones,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        g_last_cuda_error = cudaErrorInvalidValue;
+        return BITCOS_ERR_CUDA;
+    }
+    return BITCOS_OK;
+}
+
+template <int N, bool TOK, bool GROUPED>
+int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_rows, const Fp8Args &args, int64_t blocks, cudaStream_t stream) {
+    using L = Layout<N, TOK, GROUPED>;
+    static_assert(TOK || 2 * (L::kDynamic + 1024) <= 228 * 1024, "two blocks per multiprocessor");
+    static_assert(L::kDynamic <= 227 * 1024, "shared memory of a block");
+    CUtensorMap wmap, xmap;
+    int rc = encode(&wmap, W, K, args.M, experts, L::kWRowsPerTile);
+    if (rc) return rc;
+    rc = encode(&xmap, x, K, x_rows, 0, GROUPED ? 1 : L::kRowsPerTile);
+    if (rc) return rc;
+    auto *kernel = fp8_matmul_kernel<N, TOK, GROUPED>;
+    static bool prepared[32];                // (per device; as in prepare_kernel, and all of the cache as shared memory)
+    int dev = 0;
+    rc = check_cuda(cudaGetDevice(&dev));
+    if (rc) return rc;
+    if (dev >= 32 || !prepared[dev]) {
+        rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kDynamic)));
+        if (rc == BITCOS_OK)
+            rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+        if (rc) return rc;
+        if (dev < 32) prepared[dev] = true;
+    }
+    static const char *env = std::getenv("BITCOS_PDL");
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(L::kThreads);
+    cfg.dynamicSmemBytes = L::kDynamic;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(args.splits);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = args.splits > 1 ? attr : attr + 1;
+    cfg.numAttrs = (args.splits > 1 ? 1 : 0) + ((env && env[0] == '0') ? 0 : 1);
+    void *pointers[] = {&wmap, &xmap, const_cast<Fp8Args *>(&args)};
+    return check_cuda(cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(kernel), pointers));
+}
+
+int multiprocessors(int *sms) {
+    static int cache[32];
+    int dev = 0;
+    int rc = check_cuda(cudaGetDevice(&dev));
+    if (rc) return rc;
+    if (dev < 32 && cache[dev] > 0) {
+        *sms = cache[dev];
+        return BITCOS_OK;
+    }
+    rc = check_cuda(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+    if (rc == BITCOS_OK && dev < 32) cache[dev] = *sms;
+    return rc;
+}
+
+// Dense, weights first: as many shares of K as fill two blocks per multiprocessor, two groups of 128 each at least.
+template <int N>
+int launch_weights_first(const void *W, const void *x, int64_t K, Fp8Args &a, int sms, cudaStream_t stream) {
+    const int64_t row_tiles = (a.rows + N - 1) / N, tiles = row_tiles * a.w_blocks;
+    if (tiles > INT_MAX / kMaxSplits) return BITCOS_ERR_SHAPE;
+    a.row_tiles = static_cast<int>(row_tiles);
+    a.w_tiles = a.w_blocks;
+    a.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, a.G / 2, 2 * sms / tiles})));
+    return launch_fp8<N, false, false>(W, x, K, 1, a.rows, a, tiles * a.splits, stream);
+}
+
+int status_word(void *workspace, size_t workspace_bytes, unsigned int **status) {
+    *status = static_cast<unsigned int *>(workspace);
+    if (!workspace) return BITCOS_OK;
+    if (!aligned16(workspace)) return BITCOS_ERR_ALIGN;
+    return workspace_bytes < BITCOS_FP8_WORKSPACE_BYTES ? BITCOS_ERR_CAPACITY : BITCOS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int bitcos_fp8_quantize(const void *x, int x_type, int64_t rows, int64_t K, uint8_t *q, float *scale, void *cuda_stream) {
+    if (!x || !q || !scale) return BITCOS_ERR_NULL;
+    if (rows < 0 || K < kGroup || K % kGroup != 0 || (x_type != BITCOS_FP32 && x_type != BITCOS_BF16)) return BITCOS_ERR_SHAPE;
+    const int64_t per_block = 16 * kQuantGroups;
+    if (rows > INT_MAX || K / kGroup > INT_MAX || rows * (K / kGroup) > per_block * INT_MAX) return BITCOS_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(q) || reinterpret_cast<uintptr_t>(scale) % 4) return BITCOS_ERR_ALIGN;
+    if (rows == 0) return BITCOS_OK;
+    const int64_t n_groups = rows * (K / kGroup);
+    const dim3 grid(static_cast<unsigned>((n_groups + per_block - 1) / per_block));
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (x_type == BITCOS_FP32) return launch_pdl(fp8_quantize_kernel<float>, grid, 256, 0, stream, static_cast<const float *>(x), q, scale, n_groups);
+    return launch_pdl(fp8_quantize_kernel<__nv_bfloat16>, grid, 256, 0, stream, static_cast<const __nv_bfloat16 *>(x), q, scale, n_groups);
+}
+
+int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t K, const uint8_t *x, const float *x_scale, int64_t rows,
+                      void *y, int y_type, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!W || !w_scale || !x || !x_scale || !y) return BITCOS_ERR_NULL;
+    if (M < 1 || M > BITCOS_FP8_ROWS_MAX || K < kGroup || K % kGroup != 0 || K > BITCOS_FP8_ROWS_MAX || rows < 0 || rows > BITCOS_FP8_ROWS_MAX ||
+        (y_type != BITCOS_FP32 && y_type != BITCOS_BF16))
+        return BITCOS_ERR_SHAPE;
+    if (!aligned16(W) || !aligned16(x) || !aligned16(y) || reinterpret_cast<uintptr_t>(w_scale) % 4 || reinterpret_cast<uintptr_t>(x_scale) % 4)
+        return BITCOS_ERR_ALIGN;
+    Fp8Args a{};
+    int rc = status_word(workspace, workspace_bytes, &a.status);
+    if (rc) return rc;
+    if (rows == 0) return BITCOS_OK;
+    a.w_scale = w_scale;
+    a.x_scale = x_scale;
+    a.y = y;
+    a.M = M;
+    a.rows = rows;
+    a.G = static_cast<int>(K / kGroup);
+    a.w_blocks = static_cast<int>((M + kGroup - 1) / kGroup);
+    a.out_bf16 = y_type == BITCOS_BF16;
+    a.vector = M % (a.out_bf16 ? 8 : 4) == 0;
+    a.splits = 1;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    int sms = 0;
+    rc = multiprocessors(&sms);
+    if (rc) return rc;
+    const int64_t row_tiles = (rows + kARows - 1) / kARows, w_tiles = (M + 255) / 256;
+    if (rows > 128 && row_tiles * w_tiles >= sms / 2) {
+        if (row_tiles * w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
+        a.row_tiles = static_cast<int>(row_tiles);
+        a.w_tiles = static_cast<int>(w_tiles);
+        return launch_fp8<256, true, false>(W, x, K, 1, rows, a, std::min<int64_t>(row_tiles * w_tiles, sms), stream);
+    }
+    if (rows <= 16) return launch_weights_first<16>(W, x, K, a, sms, stream);
+    if (rows <= 32) return launch_weights_first<32>(W, x, K, a, sms, stream);
+    if (rows <= 64) return launch_weights_first<64>(W, x, K, a, sms, stream);
+    return launch_weights_first<128>(W, x, K, a, sms, stream);
+}
+
+int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_experts, int64_t M, int64_t K, const int32_t *group_expert,
+                              const int32_t *group_begin, const int32_t *n_groups_device, int max_groups, const int32_t *pair_xrow,
+                              int64_t n_pairs, const uint8_t *x, const float *x_scale, int64_t n_xrows, void *y, int y_type, void *workspace,
+                              size_t workspace_bytes, void *cuda_stream) {
+    if (!W || !w_scale || !group_expert || !group_begin || !n_groups_device || !x || !x_scale || !y) return BITCOS_ERR_NULL;
+    if (M < 1 || M > BITCOS_FP8_ROWS_MAX || K < kGroup || K % kGroup != 0 || K > BITCOS_FP8_ROWS_MAX || n_experts < 1 || max_groups < 1 ||
+        max_groups > kMaxGroups || n_pairs < 0 || n_pairs > BITCOS_FP8_ROWS_MAX || n_xrows < 1 || n_xrows > BITCOS_FP8_ROWS_MAX ||
+        (y_type != BITCOS_FP32 && y_type != BITCOS_BF16))
+        return BITCOS_ERR_SHAPE;
+    if (!aligned16(W) || !aligned16(x) || !aligned16(y) || reinterpret_cast<uintptr_t>(w_scale) % 4 || reinterpret_cast<uintptr_t>(x_scale) % 4 ||
+        reinterpret_cast<uintptr_t>(group_expert) % 4 || reinterpret_cast<uintptr_t>(group_begin) % 4 ||
+        reinterpret_cast<uintptr_t>(n_groups_device) % 4 || reinterpret_cast<uintptr_t>(pair_xrow) % 4)
+        return BITCOS_ERR_ALIGN;
+    Fp8Args a{};
+    int rc = status_word(workspace, workspace_bytes, &a.status);
+    if (rc) return rc;
+    if (n_pairs == 0) return BITCOS_OK;
+    a.w_scale = w_scale;
+    a.x_scale = x_scale;
+    a.y = y;
+    a.M = M;
+    a.rows = n_pairs;
+    a.G = static_cast<int>(K / kGroup);
+    a.w_blocks = static_cast<int>((M + kGroup - 1) / kGroup);
+    a.out_bf16 = y_type == BITCOS_BF16;
+    a.vector = M % (a.out_bf16 ? 8 : 4) == 0;
+    a.splits = 1;
+    a.group_expert = group_expert;
+    a.group_begin = group_begin;
+    a.n_groups = n_groups_device;
+    a.pair_xrow = pair_xrow;
+    a.max_groups = max_groups;
+    a.n_experts = n_experts;
+    a.n_xrows = static_cast<int>(n_xrows);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    int sms = 0;
+    rc = multiprocessors(&sms);
+    if (rc) return rc;
+    // what the host knows of the groups' lengths is their mean, if all of them are there
+    const int64_t mean = (n_pairs + max_groups - 1) / max_groups;
+    a.w_tiles = a.w_blocks;
+    // (no more blocks than there can be tiles)
+    const int64_t most = [&](int64_t rows) { return (n_pairs / rows + std::min<int64_t>(max_groups, n_pairs)) * a.w_tiles; }(16);
+    const int64_t two = std::min<int64_t>(2 * sms, most);
+    if (mean <= 8) return launch_fp8<16, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
+    if (mean <= 16) return launch_fp8<32, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
+    if (mean <= 32) return launch_fp8<64, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
+    if (mean <= 64) return launch_fp8<128, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
+    a.w_tiles = static_cast<int>((M + 255) / 256);
+    return launch_fp8<256, true, true>(W, x, K, n_experts, n_xrows, a, sms, stream);
+}
+
+}  // extern "C"

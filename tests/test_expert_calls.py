@@ -69,3 +69,50 @@ def test_combine_refusals():
     for change in (dict(y=8), dict(out=8), dict(base=8), dict(slot=18), dict(weight=18)):
         assert combine(**change) == ALIGN
     assert combine(tokens=0) == 0
+
+
+def fp8(**kw):
+    a = dict(W=16, w_scale=16, M=256, K=256, x=16, x_scale=16, rows=4, y=16, y_type=0, ws=0, ws_bytes=0)
+    a.update(kw)
+    p = C.c_void_p
+    return bc.load_library().bitcos_fp8_matmul(p(a["W"]), p(a["w_scale"]), a["M"], a["K"], p(a["x"]), p(a["x_scale"]), a["rows"], p(a["y"]), a["y_type"],
+                                               p(a["ws"]), a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("change,want", [(dict(W=0), NULL), (dict(w_scale=0), NULL), (dict(x=0), NULL), (dict(x_scale=0), NULL), (dict(y=0), NULL),
+                                         (dict(M=0), SHAPE), (dict(K=0), SHAPE), (dict(K=100), SHAPE), (dict(K=192), SHAPE), (dict(rows=-1), SHAPE),
+                                         (dict(M=1 << 31), SHAPE), (dict(K=1 << 31), SHAPE), (dict(rows=1 << 31), SHAPE), (dict(y_type=2), SHAPE),
+                                         (dict(W=8), ALIGN), (dict(x=8), ALIGN), (dict(y=8), ALIGN), (dict(x_scale=18), ALIGN), (dict(w_scale=18), ALIGN),
+                                         (dict(ws=8, ws_bytes=256), ALIGN), (dict(ws=16, ws_bytes=255), CAPACITY), (dict(rows=0), 0)])
+def test_fp8_matmul_refusals(change, want):
+    assert fp8(**change) == want
+
+
+def grouped(**kw):
+    a = dict(W=16, w_scale=16, E=4, M=256, K=256, ge=16, gb=16, ng=16, max_groups=4, xrow=16, pairs=8, x=16, x_scale=16, xrows=4, y=16, y_type=0, ws=0, ws_bytes=0)
+    a.update(kw)
+    p = C.c_void_p
+    return bc.load_library().bitcos_fp8_matmul_grouped(p(a["W"]), p(a["w_scale"]), a["E"], a["M"], a["K"], p(a["ge"]), p(a["gb"]), p(a["ng"]),
+                                                       a["max_groups"], p(a["xrow"]), a["pairs"], p(a["x"]), p(a["x_scale"]), a["xrows"], p(a["y"]),
+                                                       a["y_type"], p(a["ws"]), a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("change,want", [(dict(W=0), NULL), (dict(ge=0), NULL), (dict(gb=0), NULL), (dict(ng=0), NULL), (dict(x=0), NULL), (dict(y=0), NULL),
+                                         (dict(E=0), SHAPE), (dict(max_groups=0), SHAPE), (dict(max_groups=1025), SHAPE), (dict(pairs=-1), SHAPE),
+                                         (dict(pairs=1 << 31), SHAPE), (dict(xrows=0), SHAPE), (dict(M=0), SHAPE), (dict(K=64), SHAPE), (dict(y_type=2), SHAPE),
+                                         (dict(W=8), ALIGN), (dict(x=8), ALIGN), (dict(y=8), ALIGN), (dict(ge=18), ALIGN), (dict(xrow=18), ALIGN),
+                                         (dict(ws=16, ws_bytes=255), CAPACITY), (dict(pairs=0), 0)])
+def test_fp8_grouped_refusals(change, want):
+    assert grouped(**change) == want
+
+
+def test_fp8_quantize_refusals():
+    p = C.c_void_p
+
+    def call(x=16, x_type=0, rows=4, K=256, q=16, scale=16):
+        return bc.load_library().bitcos_fp8_quantize(p(x), x_type, rows, K, p(q), p(scale), None)
+
+    assert [call(x=0), call(q=0), call(scale=0)] == [NULL] * 3
+    assert [call(x_type=2), call(rows=-1), call(K=100), call(K=0), call(rows=1 << 31)] == [SHAPE] * 5
+    assert [call(x=8), call(q=8), call(scale=18)] == [ALIGN] * 3
+    assert call(rows=0) == 0
