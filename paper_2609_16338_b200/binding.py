@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -898,6 +899,7 @@ def bitcos_gemv_host(W: DeviceBitcos, x_host: np.ndarray, x_scale_host: np.ndarr
 # around the experts' products: routing, grouping of long lists, the sum over experts
 # ---------------------------------------------------------------------------------------------
 _SCORES = {"softmax": 0, "sigmoid": 1}
+_FLOAT32, _INT32 = struct.Struct("f"), struct.Struct("i")
 _type_codes = None
 
 
@@ -911,6 +913,18 @@ def _type_code(dtype, allowed, what):
     if code not in allowed:
         raise ValueError(f"{what} cannot be {dtype}")
     return code
+
+
+_empty_strided = None
+
+
+def _matrix(rows, columns, dtype, device):
+    """An uninitialised [rows, columns] tensor (torch.empty takes 1 us more to say the same)."""
+    global _empty_strided
+    if _empty_strided is None:
+        import torch
+        _empty_strided = torch.empty_strided
+    return _empty_strided((rows, columns), (columns, 1), dtype=dtype, device=device)
 
 
 def _require(ok, what):
@@ -933,19 +947,21 @@ def bitcos_route_experts(logits, top_k: int, bias=None, score: str = "softmax", 
     code = _type_code(logits.dtype, (0, 1, 2), "logits")
     stream = _stream_of(logits, bias)
     _require(1 <= top_k <= 32, "top_k must be 1 to 32")
-    out = torch.empty((3, tokens, top_k), dtype=torch.int32, device=logits.device)
-    expert, weight, xrow = out.unbind(0)
+    device = logits.device
+    expert, weight = _matrix(tokens, top_k, torch.int32, device), _matrix(tokens, top_k, torch.float32, device)
+    xrow = torch.empty_strided((tokens * top_k,), (1,), dtype=torch.int32, device=device)
     status = (_calls or _native()).bitcos_route_experts(
         logits.data_ptr(), code, max(logits.stride(0), experts) if tokens <= 1 else logits.stride(0), 0 if bias is None else bias.data_ptr(),
         tokens, experts, _SCORES[score], n_groups, top_groups, group_best, top_k, int(bool(renormalise)),
         _float_bits(scale), expert.data_ptr(), weight.data_ptr(), xrow.data_ptr(), stream) if tokens else 0
     if status:
         _check(status, "bitcos_route_experts")
-    return expert, weight.view(torch.float32), xrow.view(-1)
+    return expert, weight, xrow
 
 
 def _float_bits(v: float) -> int:
-    return C.c_int32.from_buffer(C.c_float(v)).value
+    """The bits of v as a 32-bit float (how a float passes csrc/calls.c)."""
+    return _INT32.unpack(_FLOAT32.pack(v))[0]
 
 
 def make_group_workspace(n_pairs: int, n_experts: int, device="cuda"):
@@ -966,14 +982,16 @@ def bitcos_group_pairs_slots(expert, n_experts: int, workspace=None):
     if workspace is None:
         workspace = make_group_workspace(P, n_experts, expert.device)
     cap = min(P, n_experts)
-    lists = torch.empty(2 * cap + 3 * P + 2, dtype=torch.int32, device=expert.device)
-    ge, gb, xr, order, slot, ng = lists.split((cap, cap + 1, P, P, P, 1))
+    # (the call writes all of every list; one allocation for five of them, slot keeps its shape in one of its own)
+    lists = torch.empty_strided((2 * cap + 2 * P + 2,), (1,), dtype=torch.int32, device=expert.device)
+    ge, gb, xr, order, ng = lists.split((cap, cap + 1, P, P, 1))
+    slot = _matrix(tokens, top_k, torch.int32, expert.device)
     status = (_calls or _native()).bitcos_group_pairs_slots(
         expert.data_ptr(), P, top_k, n_experts, ge.data_ptr(), gb.data_ptr(), xr.data_ptr(), order.data_ptr(), slot.data_ptr(), ng.data_ptr(),
         workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream)
     if status:
         _check(status, "bitcos_group_pairs_slots")
-    return ge, gb, xr, order, slot.view(tokens, top_k), ng
+    return ge, gb, xr, order, slot, ng
 
 
 def bitcos_combine_pairs(y, slot, weight, base=None, out=None, out_dtype=None):
@@ -987,7 +1005,7 @@ def bitcos_combine_pairs(y, slot, weight, base=None, out=None, out_dtype=None):
     tokens, top_k = slot.shape
     rows, M = y.shape
     if out is None:
-        out = torch.empty((tokens, M), dtype=out_dtype or (y if base is None else base).dtype, device=y.device)
+        out = _matrix(tokens, M, out_dtype or (y if base is None else base).dtype, y.device)
     _require(out.shape == (tokens, M) and out.is_contiguous() and (out_dtype is None or out.dtype == out_dtype), "out must be a contiguous [tokens, M] tensor")
     _require(base is None or (base.shape == out.shape and base.dtype == out.dtype and base.is_contiguous()), "base must be shaped and typed as out")
     y_code, out_code = _type_code(y.dtype, (0, 1), "y"), _type_code(out.dtype, (0, 1), "out")
@@ -1039,9 +1057,9 @@ def bitcos_fp8_quantize(x, q=None, scale=None):
     rows, K = x.shape
     code = _type_code(x.dtype, (0, 1), "x")
     if q is None:
-        q = torch.empty((rows, K), dtype=torch.float8_e4m3fn, device=x.device)
+        q = _matrix(rows, K, torch.float8_e4m3fn, x.device)
     if scale is None:
-        scale = torch.empty((rows, K // GROUP), dtype=torch.float32, device=x.device)
+        scale = _matrix(rows, K // GROUP, torch.float32, x.device)
     _require(q.dtype == torch.float8_e4m3fn and q.shape == x.shape and q.is_contiguous(), "q must be a contiguous float8_e4m3fn tensor shaped as x")
     _require(scale.dtype == torch.float32 and scale.shape == (rows, K // GROUP) and scale.is_contiguous(), "scale must be contiguous float32 [rows, K / 128]")
     stream = _stream_of(x, q, scale)
@@ -1058,7 +1076,7 @@ def _fp8_operands(W, x, x_scale, rows_out, y, out_dtype, workspace):
     _require(x_scale.dtype == torch.float32 and x_scale.shape == (x.shape[0], W.K // GROUP) and x_scale.is_contiguous(),
              "x_scale must be a contiguous float32 [rows, K / 128] tensor")
     if y is None:
-        y = torch.empty((rows_out, W.M), dtype=out_dtype or torch.float32, device=x.device)
+        y = _matrix(rows_out, W.M, out_dtype or torch.float32, x.device)
     _require(y.shape == (rows_out, W.M) and y.is_contiguous() and (out_dtype is None or y.dtype == out_dtype), "y must be a contiguous [rows, M] tensor")
     return y, _type_code(y.dtype, (0, 1), "y")
 

@@ -26,7 +26,7 @@ constexpr uint32_t kFull = 0xFFFFFFFFu;
 //
 // Which expert is taken must not hang on how exp is rounded.  Without a bias (and without sums of scores for the groups)
 // the order of the scores is the order of the logits, and that is what is compared.  Otherwise c is formed in 32 bits with
-// a bound on its error; where two choices whose order matters lie closer than their bounds, the warp does the
+// a bound on its error; where two choices whose order matters lie closer than that allows, the warp does the
 // token once more in 64 bits (route_exact).
 // ---------------------------------------------------------------------------------------------
 constexpr int kRouteWarps = 4;
@@ -44,24 +44,33 @@ struct RouteArgs {
     int n_groups, top_groups, group_best, group_size;
     int softmax, renormalise, by_choice;   // by_choice: the order of c, else of the logits
     int vector;                 // rows may be read V values at a time
+    int vector_bias;            // four biases at a time
+    int segment;                // lanes per group where that is a whole power of two, else 0
 };
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 
-// a value -> an unsigned with the same order; 0 stands for "not to be taken" (below every finite value's)
+// A value as an unsigned with the same order; 0 stands for "not to be taken" (below every finite value's).
 __device__ __forceinline__ uint32_t ordered(float v) {
-    const uint32_t b = __float_as_uint(v);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+    const int32_t b = __float_as_int(v);
+    return static_cast<uint32_t>(b ^ ((b >> 31) | INT32_MIN));
 }
 __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
-
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, d));
-    return v;
+__device__ __forceinline__ uint64_t ordered(double v) {
+    const int64_t b = __double_as_longlong(v);
+    return static_cast<uint64_t>(b ^ ((b >> 63) | INT64_MIN));
 }
+__device__ __forceinline__ double unordered(uint64_t o) {
+    return __longlong_as_double(static_cast<long long>(o >> 63 ? o & ~(1ull << 63) : ~o));
+}
+__device__ __forceinline__ uint32_t warp_max(uint32_t v) { return __reduce_max_sync(kFull, v); }
+__device__ __forceinline__ uint64_t warp_max(uint64_t v) {
+    const uint32_t hi = static_cast<uint32_t>(v >> 32), top = __reduce_max_sync(kFull, hi);
+    return (static_cast<uint64_t>(top) << 32) | __reduce_max_sync(kFull, hi == top ? static_cast<uint32_t>(v) : 0u);
+}
+
 template <typename T>
 __device__ __forceinline__ T warp_sum(T v) {
 #pragma unroll
@@ -75,90 +84,206 @@ __device__ __forceinline__ float clean(float z) {
     return fminf(z, FLT_MAX) + 0.0f;
 }
 
-// The two largest of a stream of values.
-template <typename T>
-struct Two {
-    T a, b;
-    __device__ __forceinline__ void add(T v) {
-        if (v > a) {
-            b = a;
-            a = v;
-        } else if (v > b) {
-            b = v;
+// Lane g < n_groups holds the value of group g: which groups stay, one bit each.
+template <typename F>
+__device__ __forceinline__ uint32_t kept_groups(const RouteArgs &a, F mine, int lane) {
+    int ahead = 0;
+    for (int g = 0; g < a.n_groups; ++g) {
+        const F other = __shfl_sync(kFull, mine, g);
+        ahead += other > mine || (other == mine && g < lane);
+    }
+    return __ballot_sync(kFull, lane < a.n_groups && ahead < a.top_groups);
+}
+
+// Calls f(v, the group of expert lane * V + v).
+template <int V, typename Do>
+__device__ __forceinline__ void each_group(const RouteArgs &a, int lane, Do f) {
+    int at = lane * V / a.group_size, in = lane * V - at * a.group_size;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        f(v, at);
+        if (++in == a.group_size) {
+            in = 0;
+            ++at;
         }
     }
-};
+}
 
-// The whole token in 64 bits: lane j < top_k gets the expert of place j (-1: none is left).  Rare, so short rather than fast.
+// The two largest keys of a set, joined with the two largest of the lane d away.
+template <typename K>
+__device__ __forceinline__ void add_key(K &one, K &two, K k) {
+    two = max(two, min(one, k));
+    one = max(one, k);
+}
+template <typename K>
+__device__ __forceinline__ void join_keys(K &one, K &two, int d) {
+    const K other = __shfl_xor_sync(kFull, one, d), second = __shfl_xor_sync(kFull, two, d);
+    two = max(min(one, other), max(two, second));
+    one = max(one, other);
+}
+// (key 0 has no value; `low`: bits of a key that are not part of it)
+template <typename K>
+__device__ __forceinline__ auto value_of(const RouteArgs &a, K one, K two, K low) {
+    decltype(unordered(one)) none = -INFINITY, v = one ? unordered(one & ~low) : none;
+    if (a.group_best == 2) v += two ? unordered(two & ~low) : none;
+    return v;
+}
+
+// The value of every group (lane g: group g) from the experts' keys.
+template <int V>
+__device__ __forceinline__ float group_values(const RouteArgs &a, const uint32_t (&key)[V], uint32_t low, int lane) {
+    float mine = -INFINITY;
+    if (a.segment) {
+        // every group is the whole runs of a power of two of lanes
+        uint32_t one = 0, two = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) add_key(one, two, key[v]);
+        for (int d = 1; d < a.segment; d <<= 1) join_keys(one, two, d);
+        mine = __shfl_sync(kFull, value_of(a, one, two, low), lane * a.segment & 31);
+    } else {
+        for (int g = 0; g < a.n_groups; ++g) {
+            uint32_t one = 0, two = 0;
+            each_group<V>(a, lane, [&](int v, int at) {
+                if (at == g) add_key(one, two, key[v]);
+            });
+#pragma unroll
+            for (int d = 16; d; d >>= 1) join_keys(one, two, d);
+            if (lane == g) mine = value_of(a, one, two, low);
+        }
+    }
+    return mine;
+}
+
+// The choice of an expert of logit z in 64 bits.  (Few tokens come here, one at a time, and each waits for every instruction to
+// be fetched: what follows stays loops and calls; unrolled, a token took 15 us.)
+__device__ __noinline__ double exact_choice(const RouteArgs &a, double z, int e, double top, double sum) {
+    if (!a.by_choice) return z;
+    const double p = exp(a.softmax ? z - top : -z);
+    const float b = a.bias ? clean(__ldg(a.bias + e)) : 0.f;
+    return (a.softmax ? p : 1.0) / (a.softmax ? sum : 1.0 + p) + static_cast<double>(b) + 0.0;
+}
+
+// The sum under the softmax in 64 bits.
 template <int V, typename L>
-__device__ __noinline__ int route_exact(const RouteArgs &a, const L *row, int lane) {
-    double c[V];
-    double top = -INFINITY, sum = 0.0;
+__device__ __noinline__ double exact_sum(const RouteArgs &a, const L *row, int lane, double top) {
+    double sum = 0.0;
+#pragma unroll 1
     for (int v = 0; v < V; ++v) {
         const int e = lane * V + v;
-        c[v] = e < a.experts ? static_cast<double>(clean(to_float(row[e]))) : -INFINITY;
-        top = fmax(top, c[v]);
+        if (e < a.experts) sum += exp(static_cast<double>(clean(to_float(row[e]))) - top);
     }
-    if (a.softmax) {
-        for (int d = 16; d; d >>= 1) top = fmax(top, __shfl_xor_sync(kFull, top, d));
-        for (int v = 0; v < V; ++v) sum += c[v] > -INFINITY ? exp(c[v] - top) : 0.0;
-        sum = warp_sum(sum);
+    return warp_sum(sum);
+}
+
+// The places of n <= 32 candidates (lane j < n: expert e), among which all that will be taken are: lane j < top_k gets the expert of
+// place j.
+template <int V, typename L>
+__device__ __noinline__ int order_candidates(const RouteArgs &a, const L *row, int lane, float top, int e, int n) {
+    const double sum = a.by_choice && a.softmax ? exact_sum<V, L>(a, row, lane, top) : 1.0;
+    const bool is = lane < n;
+    const double c = is ? exact_choice(a, static_cast<double>(clean(to_float(row[e]))), e, top, sum) : 0.0;
+    int place = 0;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        const double other = __shfl_sync(kFull, c, i);
+        const int index = __shfl_sync(kFull, e, i);
+        place += other > c || (other == c && index < e);
     }
+    int taken = -1;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        const int at = __shfl_sync(kFull, place, i), index = __shfl_sync(kFull, e, i);
+        if (lane == at && lane < a.top_k) taken = index;
+    }
+    return taken;
+}
+
+// The whole token in 64 bits: lane j < top_k gets the expert of place j (-1: none is left).
+template <int V, typename L>
+__device__ __noinline__ int route_exact(const RouteArgs &a, const L *row, int lane, float top) {
+    uint64_t key[V];
+    const double sum = a.by_choice && a.softmax ? exact_sum<V, L>(a, row, lane, top) : 1.0;
+#pragma unroll 1
     for (int v = 0; v < V; ++v) {
         const int e = lane * V + v;
-        if (!(c[v] > -INFINITY)) continue;
-        const double s = a.softmax ? exp(c[v] - top) / sum : 1.0 / (1.0 + exp(-c[v]));
-        const float b = a.bias ? clean(a.bias[e]) : 0.0f;
-        c[v] = s + static_cast<double>(b);
+        const float z = e < a.experts ? clean(to_float(row[e])) : -INFINITY;
+        const bool there = z > -INFINITY && (!a.by_choice || !a.bias || clean(__ldg(a.bias + e)) > -INFINITY);
+        key[v] = there ? ordered(exact_choice(a, z, e, top, sum)) : 0;
     }
     if (a.n_groups > 1) {
-        double mine = -INFINITY;                             // lane g: the value of group g
-        for (int g = 0; g < a.n_groups; ++g) {
-            Two<double> t{-INFINITY, -INFINITY};
-            for (int v = 0; v < V; ++v)
-                if ((lane * V + v) / a.group_size == g && lane * V + v < a.experts) t.add(c[v]);
-            for (int d = 16; d; d >>= 1) {
-                const double oa = __shfl_xor_sync(kFull, t.a, d), ob = __shfl_xor_sync(kFull, t.b, d);
-                t.b = fmax(fmin(t.a, oa), fmax(t.b, ob));
-                t.a = fmax(t.a, oa);
+        double mine = -INFINITY;
+        if (a.segment) {
+            uint64_t one = 0, two = 0;
+#pragma unroll 1
+            for (int v = 0; v < V; ++v) add_key(one, two, key[v]);
+#pragma unroll 1
+            for (int d = 1; d < a.segment; d <<= 1) join_keys(one, two, d);
+            mine = __shfl_sync(kFull, value_of(a, one, two, uint64_t(0)), lane * a.segment & 31);
+        } else {
+#pragma unroll 1
+            for (int g = 0; g < a.n_groups; ++g) {
+                uint64_t one = 0, two = 0;
+                const int from = max(g * a.group_size - lane * V, 0), to = min((g + 1) * a.group_size - lane * V, V);
+#pragma unroll 1
+                for (int v = from; v < to; ++v) add_key(one, two, key[v]);
+#pragma unroll 1
+                for (int d = 16; d; d >>= 1) join_keys(one, two, d);
+                if (lane == g) mine = value_of(a, one, two, uint64_t(0));
             }
-            const double value = a.group_best == 2 ? t.a + t.b : t.a;
-            if (lane == g) mine = value;
         }
-        int ahead = 0;
-        for (int g = 0; g < a.n_groups; ++g) {
-            const double other = __shfl_sync(kFull, mine, g);
-            ahead += other > mine || (other == mine && g < lane);
-        }
-        const uint32_t kept = __ballot_sync(kFull, lane < a.n_groups && ahead < a.top_groups);
+        const uint32_t kept = kept_groups(a, mine, lane);
+        int at = lane * V / a.group_size, in = lane * V - at * a.group_size;
+#pragma unroll 1
         for (int v = 0; v < V; ++v) {
-            const int e = lane * V + v;
-            if (e >= a.experts || !((kept >> (e / a.group_size)) & 1u)) c[v] = -INFINITY;
+            if (at >= a.n_groups || !((kept >> at) & 1u)) key[v] = 0;
+            if (++in == a.group_size) {
+                in = 0;
+                ++at;
+            }
         }
     }
     int taken = -1;
+    bool look = true;                        // this lane's best is to be found (anew)
+    uint64_t best = 0;
+    int at = 0;
+#pragma unroll 1
     for (int j = 0; j < a.top_k; ++j) {
-        double best = -INFINITY;
-        int at = INT_MAX;
-        for (int v = 0; v < V; ++v)
-            if (c[v] > best) {
-                best = c[v];
-                at = lane * V + v;
-            }
-        for (int d = 16; d; d >>= 1) {
-            const double ob = __shfl_xor_sync(kFull, best, d);
-            const int oat = __shfl_xor_sync(kFull, at, d);
-            if (ob > best || (ob == best && oat < at)) {
-                best = ob;
-                at = oat;
-            }
+        if (look) {
+            best = 0;
+#pragma unroll 1
+            for (int v = 0; v < V; ++v)
+                if (key[v] > best) {
+                    best = key[v];
+                    at = v;
+                }
         }
-        if (at == INT_MAX) break;                            // (the same on every lane)
-        for (int v = 0; v < V; ++v)
-            if (lane * V + v == at) c[v] = -INFINITY;
-        if (lane == j) taken = at;
+        const uint64_t all = warp_max(best);
+        if (all == 0) break;
+        const int winner = __ffs(__ballot_sync(kFull, best == all)) - 1;      // (lowest lane = lowest expert)
+        const int e = __shfl_sync(kFull, lane * V + at, winner);
+        look = lane == winner;
+        if (look) key[at] = 0;
+        if (lane == j) taken = e;
     }
     return taken;
+}
+
+// Sorts the keys of a lane, largest first (Batcher's odd-even merge sort).
+template <int V>
+__device__ __forceinline__ void sort_keys(uint32_t (&key)[V]) {
+#pragma unroll
+    for (int p = 1; p < V; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int j = k % p; j + k < V; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < V && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const uint32_t hi = max(key[i + j], key[i + j + k]), lo = min(key[i + j], key[i + j + k]);
+                        key[i + j] = hi;
+                        key[i + j + k] = lo;
+                    }
 }
 
 template <int V, typename L>
@@ -191,158 +316,151 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const __grid_co
             z[v] = e < a.experts ? clean(to_float(row[e])) : -INFINITY;
         }
     }
-    float top = 0.f, sum = 1.f;
+    float most = z[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) most = fmaxf(most, z[v]);
+    const float top = unordered(warp_max(ordered(most)));      // (-inf: nothing is left)
+    uint32_t key[V];
+    float sum = 1.f;
     if (a.softmax) {
-        top = z[0];
-#pragma unroll
-        for (int v = 1; v < V; ++v) top = fmaxf(top, z[v]);
-        top = warp_max(top);
         sum = 0.f;
-        if (top > -INFINITY) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) sum += expf(z[v] - top);      // (a masked one: exp(-inf) = 0)
+        for (int v = 0; v < V; ++v) {
+            const float e = top > -INFINITY ? expf(z[v] - top) : 0.f;          // (a masked one: exp(-inf) = 0)
+            key[v] = __float_as_uint(e);
+            sum += e;
         }
         sum = warp_sum(sum);
     }
     const auto score = [&](float zz) { return a.softmax ? expf(zz - top) / sum : 1.0f / (1.0f + expf(-zz)); };
-    // bound on the error of a score s of logit zz, and with it of the choice c = s + b: exp, sum and quotient are good to
-    // 2^-20 of s, the argument's rounding adds 2^-24 of itself, the addition 2^-24 of c (bounds doubled; 1e-38: scores below the normal
-    // range, which exp may have rounded to nothing)
-    const auto error = [&](float s, float zz, float c) {
-        const float d = a.softmax ? fminf(top - zz, 128.f) : 0.f;
-        return s * (9.5367431640625e-7f + d * 1.1920929e-7f) + fabsf(c) * 1.1920929e-7f + 1e-38f;
-    };
 
-    uint32_t key[V];
-    float upper[V];                // the choice with its bound added (by_choice only)
-    bool near = false;             // an order that 32 bits cannot tell
+    // The low bits of a key say which of its lane's experts it is (V - 1 - v: of equal ones the first is the largest), so that
+    // a lane's keys can be sorted with minima and maxima alone.  For 16-bit logits nothing is lost, the bits are not used; otherwise the
+    // order is checked below, with what those bits are worth counted as an error.
+    constexpr uint32_t kLow = V - 1;
+    const auto keyed = [&](float v32, int v) { return (ordered(v32) & ~kLow) | (kLow - v); };
+    const bool inexact = a.by_choice || sizeof(L) == 4;
+    float unit = 1e-37f;           // no choice is further off than this (a logit: than rel of itself)
+    const float rel = a.by_choice ? 0.f : V * 1.1f * 1.1920929e-7f;
+    const auto apart = [&](float more, float less, float units) { return more - less > units * unit + rel * (fabsf(more) + fabsf(less)); };
     if (!a.by_choice) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = z[v] > -INFINITY ? ordered(z[v]) : 0u;
+        for (int v = 0; v < V; ++v) {
+            const bool there = z[v] > -INFINITY;
+            key[v] = there ? keyed(z[v], v) : 0u;
+        }
     } else {
+        // Only the order hangs on these scores, so the fast exponential and quotient do (2 + 1.2 |z| and 2 units of 2^-23); the
+        // weights of the taken ones are formed anew below.  Error of a score, in units of 2^-23 and of the largest score s_max
+        // of the token: softmax, s (8 + d) at d = top - z with s = s_max exp(-d), so below 9, and the V + 5 additions of the sum, half a
+        // unit each; sigmoid, s (6 + 1.2 |z|), which is largest at the top logit or near z = -1.28, so below 8 + 1.2 |top|.  Then half a
+        // unit of |c| for the addition and V for the low bits of the key; scores under the normal range may have been rounded to nothing
+        // (1e-37).  All a tenth larger.
+        const float inv = 1.0f / sum;
+        float bias[V], size = 0.f;
+        if (!a.bias) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) bias[v] = 0.f;
+        } else if (V % 4 == 0 && a.vector_bias) {
+#pragma unroll
+            for (int v = 0; v < V; v += 4) {
+                const float4 b = __ldg(reinterpret_cast<const float4 *>(a.bias + lane * V + v));
+                bias[v] = b.x, bias[(v + 1) % V] = b.y, bias[(v + 2) % V] = b.z, bias[(v + 3) % V] = b.w;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) bias[v] = lane * V + v < a.experts ? __ldg(a.bias + lane * V + v) : 0.f;
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int e = lane * V + v;
-            key[v] = 0u;
-            upper[v] = -INFINITY;
-            if (z[v] > -INFINITY) {
-                const float b = a.bias ? clean(__ldg(a.bias + e)) : 0.f;
-                if (b > -INFINITY) {
-                    const float s = score(z[v]), c = fminf(s + b, FLT_MAX) + 0.0f;
-                    key[v] = ordered(c);
-                    upper[v] = c + error(s, z[v], c);
-                }
-            }
+            const float s = a.softmax ? __uint_as_float(key[v]) * inv : __fdividef(1.0f, 1.0f + __expf(-z[v]));
+            const float c = fminf(s + bias[v], FLT_MAX);          // (fminf makes FLT_MAX of a NaN: the sum is asked)
+            const bool there = z[v] > -INFINITY && s + bias[v] > -INFINITY;
+            key[v] = there ? keyed(c, v) : 0u;
+            if (there) size = fmaxf(size, fabsf(c));
         }
+        const float s_max = a.softmax ? inv : 1.0f / (1.0f + expf(-top));
+        unit += 1.1f * 1.1920929e-7f * (s_max * (a.softmax ? 12.f + 0.5f * V : 8.f + 1.2f * fminf(fabsf(top), 100.f)) +
+                                        __uint_as_float(warp_max(__float_as_uint(size))) * (0.5f + V));
     }
 
+    bool groups_near = false;
     if (a.n_groups > 1) {
-        // lane g: the value of group g, and how far it may be off
-        float mine = -INFINITY, off = 0.f;
-        for (int g = 0; g < a.n_groups; ++g) {
-            Two<float> t{-INFINITY, -INFINITY};
-            float far = 0.f;
+        const float mine = group_values<V>(a, key, kLow, lane);
+        const uint32_t kept = kept_groups(a, mine, lane);
+        if (a.segment) {
+            if (!((kept >> (lane / a.segment)) & 1u) || lane / a.segment >= a.n_groups) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int e = lane * V + v;
-                if (key[v] && e / a.group_size == g) {
-                    const float c = unordered(key[v]);
-                    t.add(c);
-                    if (a.by_choice) far = fmaxf(far, upper[v] - c);
-                }
+                for (int v = 0; v < V; ++v) key[v] = 0u;
             }
-#pragma unroll
-            for (int d = 16; d; d >>= 1) {
-                const float oa = __shfl_xor_sync(kFull, t.a, d), ob = __shfl_xor_sync(kFull, t.b, d);
-                far = fmaxf(far, __shfl_xor_sync(kFull, far, d));
-                t.b = fmaxf(fminf(t.a, oa), fmaxf(t.b, ob));
-                t.a = fmaxf(t.a, oa);
-            }
-            const float value = a.group_best == 2 ? t.a + t.b : t.a;
-            if (lane == g) {
-                mine = value;
-                off = value > -INFINITY ? 2.f * far + fabsf(value) * 1.1920929e-7f : 0.f;
-            }
+        } else {
+            each_group<V>(a, lane, [&](int v, int at) {
+                if (at >= a.n_groups || !((kept >> at) & 1u)) key[v] = 0u;
+            });
         }
-        int ahead = 0;
-        for (int g = 0; g < a.n_groups; ++g) {
-            const float other = __shfl_sync(kFull, mine, g);
-            ahead += other > mine || (other == mine && g < lane);
-        }
-        const bool is_group = lane < a.n_groups, keep = is_group && ahead < a.top_groups;
-        const uint32_t kept = __ballot_sync(kFull, keep);
-        if (a.by_choice && a.top_groups < a.n_groups) {
-            const float low = -warp_max(keep ? off - mine : -INFINITY);
-            const float high = warp_max(is_group && !keep ? mine + off : -INFINITY);
-            near = high > -INFINITY && high >= low;
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int e = lane * V + v;
-            if (e < a.experts && !((kept >> (e / a.group_size)) & 1u)) {
-                key[v] = 0u;
-                upper[v] = -INFINITY;
-            }
+        if (inexact && a.top_groups < a.n_groups) {
+            // the smallest value of a kept group, the largest of one that is not; a value: two choices and the rounding of their sum
+            const bool keep = (kept >> lane) & 1u;
+            const float low = unordered(~warp_max(keep ? ~ordered(mine) : 0u));
+            const float high = unordered(warp_max(lane < a.n_groups && !keep ? ordered(mine) : ordered(-INFINITY)));
+            groups_near = high > -INFINITY && !apart(low, high, 6.f);
         }
     }
 
+    sort_keys<V>(key);
     int taken = -1;                // lane j: the expert of place j
     uint32_t taken_key = 0u;
-    int places = a.top_k;          // how many were found
-    for (int j = 0; j < a.top_k; ++j) {
-        uint32_t best = key[0];
-        int at = 0;
-#pragma unroll
-        for (int v = 1; v < V; ++v)
-            if (key[v] > best) {
-                best = key[v];
-                at = v;
-            }
-        const uint32_t all = __reduce_max_sync(kFull, best);
-        if (all == 0u) {
-            places = j;
-            break;
-        }
-        const int winner = __ffs(__ballot_sync(kFull, best == all)) - 1;      // (lowest lane = lowest expert)
-        const int e = __shfl_sync(kFull, lane * V + at, winner);
+    // the best of all that are left (0: none), which goes to place j if it is at least `least`
+    const auto next = [&](int j, uint32_t least) {
+        const uint32_t mine = key[0] & ~kLow, all = warp_max(mine);
+        if (all == 0u || all < least) return false;
+        const int winner = __ffs(__ballot_sync(kFull, mine == all)) - 1;      // (equal ones: the lowest lane, the lowest expert)
+        const uint32_t won = __shfl_sync(kFull, key[0], winner);
         if (lane == winner) {
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v == at) {
-                    key[v] = 0u;
-                    if (a.by_choice) upper[v] = -INFINITY;
-                }
+            for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
+            key[V - 1] = 0u;
         }
         if (lane == j) {
-            taken = e;
+            taken = winner * V + static_cast<int>(kLow - (won & kLow));
             taken_key = all;
         }
-    }
+        return true;
+    };
+    int places = 0;                // how many were found
+    while (places < a.top_k && next(places, 0u)) ++places;
 
     float zt = taken >= 0 ? clean(to_float(row[taken])) : -INFINITY;
-    float s = taken >= 0 ? score(zt) : 0.f;
-    if (a.by_choice) {
-        // the taken choices in order, every one above the next by more than their bounds (or the same logit and bias, where
+    if (inexact) {
+        // the taken ones in order, every one above the next by more than both may be off (or the same logit and bias, where
         // the lower index goes first), the last one above all that are left
         const float c = taken >= 0 ? unordered(taken_key) : 0.f;
         const float b = taken >= 0 && a.bias ? clean(__ldg(a.bias + taken)) : 0.f;
-        const float err = error(s, zt, c);
-        const float up_next = __shfl_down_sync(kFull, c + err, 1), z_next = __shfl_down_sync(kFull, zt, 1), b_next = __shfl_down_sync(kFull, b, 1);
-        bool close = lane + 1 < places && up_next >= c - err && !(z_next == zt && b_next == b);
+        const int e_next = __shfl_down_sync(kFull, taken, 1);
+        const float c_next = __shfl_down_sync(kFull, c, 1), z_next = __shfl_down_sync(kFull, zt, 1), b_next = __shfl_down_sync(kFull, b, 1);
+        bool close = lane + 1 < places && !apart(c, c_next, 2.f) && !(z_next == zt && b_next == b && taken < e_next);
         if (places == a.top_k) {
-            float left = upper[0];
-#pragma unroll
-            for (int v = 1; v < V; ++v) left = fmaxf(left, upper[v]);
-            left = warp_max(left);
-            close = close || (lane == places - 1 && left >= c - err && left > -INFINITY);
+            const uint32_t left = warp_max(key[0] & ~kLow);
+            close = close || (lane == places - 1 && left != 0u && !apart(c, unordered(left), 2.f));
         }
-        near = near || __any_sync(kFull, close);
-        if (near) {
-            taken = route_exact<V, L>(a, row, lane);
+        const bool some = __any_sync(kFull, close);
+        if (groups_near || some) {
+            // the candidates: the taken ones and what is left within reach of the last
+            int n = places;
+            bool whole = groups_near;
+            if (!whole && places == a.top_k) {
+                const float last = __shfl_sync(kFull, c, places - 1);
+                // (a value just under the border may be let in, none over it is left out)
+                const uint32_t least = ordered(last - (2.1f * unit + 2.1f * rel * fabsf(last))) & ~kLow;
+                while (n < 32 && next(n, least)) ++n;
+                const uint32_t more = warp_max(key[0] & ~kLow);
+                whole = n == 32 && more != 0u && more >= least;      // (more than a lane each)
+            }
+            taken = whole ? route_exact<V, L>(a, row, lane, top) : order_candidates<V, L>(a, row, lane, top, taken, n);
             zt = taken >= 0 ? clean(to_float(row[taken])) : -INFINITY;
-            s = taken >= 0 ? score(zt) : 0.f;
         }
     }
+    float s = taken >= 0 ? score(zt) : 0.f;
     if (a.renormalise) s = s / (warp_sum(s) + 1e-20f);
     if (lane < a.top_k) {
         const int64_t p = token * a.top_k + lane;
@@ -364,6 +482,9 @@ int launch_route_type(RouteArgs a, cudaStream_t stream) {
     while (V * 32 < a.experts) V *= 2;
     const size_t chunk = std::min<size_t>(16, V * sizeof(L));
     a.vector = a.experts == V * 32 && reinterpret_cast<uintptr_t>(a.logits) % chunk == 0 && a.row_stride * sizeof(L) % chunk == 0;
+    a.vector_bias = a.experts == V * 32 && aligned16(a.bias);
+    a.segment = 0;
+    if (a.group_size % V == 0 && (a.group_size / V & (a.group_size / V - 1)) == 0) a.segment = a.group_size / V;
     switch (V) {
         case 1: return launch_route<1, L>(a, stream);
         case 2: return launch_route<2, L>(a, stream);

@@ -147,6 +147,17 @@ def test_route_orders_that_32_bits_cannot_tell(bc):
     check_route(bc, torch.from_numpy(z).cuda(), bias, top_k=8, score="softmax")
     check_route(bc, torch.from_numpy(z).cuda(), bias, top_k=8, score="sigmoid", n_groups=8, top_groups=3, group_best=2)
     check_route(bc, torch.from_numpy(z).cuda(), None, top_k=8, score="sigmoid", n_groups=8, top_groups=3, group_best=2)
+    # more candidates at the border than a warp has lanes, and as many places as lanes
+    check_route(bc, torch.from_numpy(z).cuda(), bias, top_k=32, score="sigmoid")
+    wide = (rng.normal(0, 1e-6, (50, 300)) - 3.0).astype(np.float32)
+    level = np.ones(300, np.float32)
+    for top_k in (1, 8, 32):
+        check_route(bc, torch.from_numpy(wide).cuda(), level, top_k=top_k, score="sigmoid")
+        check_route(bc, torch.from_numpy(wide).cuda(), level, top_k=top_k, score="softmax")
+    # 32-bit logits without a bias, one unit in the last place apart
+    step = np.float32(1.0) + rng.permuted(np.tile(np.arange(500, dtype=np.float32), (40, 1)), axis=1) * np.float32(2.0 ** -23)
+    check_route(bc, torch.from_numpy(step).cuda(), None, top_k=8)
+    check_route(bc, torch.from_numpy(-step).cuda(), None, top_k=32, n_groups=4, top_groups=2)
     # equal logits and equal biases: the lower index
     check_route(bc, torch.zeros(3, E, device="cuda"), np.zeros(E, np.float32), top_k=8, score="sigmoid")
 
