@@ -10,14 +10,14 @@
 // the two scales and add in fp32 registers while the next group is being multiplied into the other accumulator.
 //
 // Two operand orders, chosen by the host (choose_dense, choose_grouped):
-//   tokens first   A = 128 tokens, B = 256 weight rows.  A promoter thread holds one token's 128 columns; the scales of a group are
+//   tokens first   A = 128 tokens, B = 256 weight rows.  A promoter thread holds 64 columns of one token; the scales of a group are
 //                  one number per thread.  Tiles are spread over persistent blocks.  For prompts.
 //   weights first  A = 128 weight rows, B = 16 .. 128 tokens.  The weights pass once for up to 128 tokens, two blocks per
 //                  multiprocessor keep enough of them in flight, and K is cut over the blocks of a cluster where there are few row
 //                  blocks: each leaves its sums in shared memory, and the cluster adds them in order of rank (no workspace, no
 //                  atomics, the same bits every time).  For decoding.
 //
-// Operands come by TMA (128-byte swizzle, 128 bytes of K per stage); the rows of routed pairs by tile::gather4.
+// Operands come by TMA (128-byte swizzle, 128 bytes of K per stage); rows of routed pairs by cp.async from two warps of their own.
 #include "bitcos.h"
 #include "common.cuh"
 
@@ -111,6 +111,7 @@ constexpr int kMaxSplits = 8;             // portable cluster size
 struct Fp8Args {
     const float *w_scale;       // [experts][w_blocks][G]
     const float *x_scale;       // [x rows][G]
+    const uint8_t *x;           // grouped: rows to gather
     void *y;
     unsigned int *status;       // NULL, or the workspace's status word
     int64_t M;
@@ -138,11 +139,13 @@ struct Layout {
     static constexpr uint32_t kBBytes = N * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = TOK ? 4 : N <= 32 ? 5 : N == 64 ? 4 : 3;
-    static constexpr int kPromoters = TOK ? 8 : 4;      // warps
-    static constexpr int kThreads = 64 + kPromoters * 32;
+    static constexpr int kPromoters = TOK ? 16 : 4;     // warps
+    static constexpr int kFirst = GROUPED ? 4 : 2;      // the first of them (in front: TMA, tensor cores, two for gathered rows)
+    static constexpr int kThreads = (kFirst + kPromoters) * 32;
+    static constexpr int kColumns = TOK ? N / 4 : N;    // of the accumulator per promoter thread
     static constexpr int kRowsPerTile = TOK ? kARows : N;
     static constexpr int kWRowsPerTile = TOK ? N : kARows;
-    static constexpr uint32_t kColumns = 2 * N < 32 ? 32 : 2 * N;
+    static constexpr uint32_t kTmemColumns = 2 * N < 32 ? 32 : 2 * N;
     // byte offsets behind the stages
     static constexpr uint32_t kBars = kStages * kStageBytes;
     static constexpr uint32_t kTmem = kBars + (2 * kStages + 4) * 8;
@@ -162,11 +165,10 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int
                  "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
                  : "memory");
 }
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int c0, const int (&r)[4], uint32_t bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-        "l"(map), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(bar)
-        : "memory");
+// 16 bytes from anywhere in global memory, asynchronously (the rows of routed pairs: one copy of a whole row's 128 bytes
+// by tile::gather4 costs the TMA unit about 25 clocks, 3300 a stage of 128 rows).
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
 // Shared-memory matrix descriptor: K-major rows of 128 bytes, 128-byte swizzle, eight rows (1024 bytes) apart per step.
@@ -281,12 +283,13 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     int64_t *prefix = reinterpret_cast<int64_t *>(smem + L::kPrefix);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int splits = GROUPED || TOK ? 1 : a.splits;
+    const bool gather = GROUPED && a.pair_xrow != nullptr;
     const int rank = splits > 1 ? static_cast<int>(cluster_rank()) : 0;
     const int k0 = static_cast<int>(static_cast<int64_t>(a.G) * rank / splits), k1 = static_cast<int>(static_cast<int64_t>(a.G) * (rank + 1) / splits);
 
     if (warp == 0 && lane == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(full + 8 * s, 1);
+            mbar_init(full + 8 * s, gather ? 3 : 1);
             mbar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -307,7 +310,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kTmem), "n"(L::kColumns) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kTmem), "n"(L::kTmemColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         tmem_fence_before();
     }
@@ -351,6 +354,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         n_tiles = prefix[n_groups];
     }
     const int64_t t_first = blockIdx.x / splits, t_step = gridDim.x / splits;
+    constexpr uint32_t kXBytes = TOK ? kABytes : L::kBBytes;
     bool ok = true;
     uint32_t it = 0;                       // groups of 128 so far, over all tiles
 
@@ -358,16 +362,6 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         // ---- producer
         for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
             const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
-            int src[4] = {0, 0, 0, 0};
-            if constexpr (GROUPED) {
-                // rows 4 lane .. + 3 of the tile; what is not a row of the tile, or no row of x, reads some row of x and is dropped later
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int i = lane * 4 + j;
-                    const int r = i < tile.rows ? (a.pair_xrow ? __ldg(a.pair_xrow + tile.row0 + i) : static_cast<int>(tile.row0 + i)) : 0;
-                    src[j] = r >= 0 && r < a.n_xrows ? r : 0;
-                }
-            }
             for (int kb = k0; ok && kb < k1; ++kb, ++it) {
                 const uint32_t s = it % kStages;
                 const uint32_t stage = base + s * L::kStageBytes, bar = full + 8 * s;
@@ -377,15 +371,12 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     break;
                 }
                 const bool sent = !GROUPED && it < kStages && t == t_first;       // (announced and the weights sent above)
-                if (lane == 0 && !sent) {
-                    mbar_expect_tx(bar, L::kStageBytes);
-                    tma_3d(w_dst, &wmap, kb * kGroup, tile.w0, tile.expert, bar);
-                }
-                if constexpr (GROUPED) {
-                    __syncwarp();
-                    if (lane < L::kRowsPerTile / 4) tma_gather4(x_dst + lane * 512, &xmap, kb * kGroup, src, bar);
-                } else if (lane == 0) {
-                    tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), bar);
+                if (lane == 0) {
+                    if (!sent) {
+                        mbar_expect_tx(bar, gather ? L::kStageBytes - kXBytes : L::kStageBytes);
+                        tma_3d(w_dst, &wmap, kb * kGroup, tile.w0, tile.expert, bar);
+                    }
+                    if (!gather) tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), bar);
                 }
             }
         }
@@ -418,12 +409,54 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             for (uint32_t i = it > 2 ? it - 2 : 0; i < it; ++i) ok &= mbar_wait(acc_full + 8 * (i & 1), (i / 2) & 1);
         }
         __syncwarp();
+    } else if (GROUPED && warp < L::kFirst) {
+        // ---- rows of routed pairs: two warps, eight lanes per row of 128 bytes, 16 bytes each, put where the 128-byte swizzle has them
+        if (gather) {
+            constexpr int kOwn = L::kRowsPerTile / 8, kLag = kStages - 2;
+            const int p = threadIdx.x - 64, r0 = p >> 3, chunk = p & 7;
+            const uint32_t x_off = (TOK ? 0 : kABytes) + r0 * kGroup + ((chunk ^ (r0 & 7)) << 4);
+            const uint8_t *x = a.x + chunk * 16;
+            const int64_t K = static_cast<int64_t>(a.G) * kGroup;
+            // a stage is handed on when its copies have landed, kLag stages later
+            const auto hand_on = [&](uint32_t i) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full + 8 * (i % kStages));
+            };
+            for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
+                const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
+                // what is not a row of the tile, or no row of x, reads row 0 and is dropped later
+                int src[kOwn];
+#pragma unroll
+                for (int j = 0; j < kOwn; ++j) {
+                    const int i = r0 + 8 * j;
+                    const int r = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : 0;
+                    src[j] = r >= 0 && r < a.n_xrows ? r : 0;
+                }
+                for (int kb = k0; kb < k1; ++kb, ++it) {
+                    const uint32_t s = it % kStages, dst = base + s * L::kStageBytes + x_off;
+                    if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
+                        ok = false;
+                        break;
+                    }
+#pragma unroll
+                    for (int j = 0; j < kOwn; ++j) copy16(dst + j * 8 * kGroup, x + src[j] * K + kb * kGroup);
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (it >= kLag) {
+                        asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+                        hand_on(it - kLag);
+                    }
+                }
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            for (uint32_t i = it > kLag ? it - kLag : 0; i < it; ++i) hand_on(i);
+        }
     } else {
         // ---- promoters: warp w of four reads lanes 32 (w % 4) .. + 31 of the accumulators
-        const int quarter = warp & 3, half = TOK ? (warp - 2) >> 2 : 0;
+        constexpr int kCols = L::kColumns;
+        const int quarter = warp & 3, part = TOK ? (warp - L::kFirst) >> 2 : 0;
         const int row = quarter * 32 + lane;       // of A
-        const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + half * 128;
-        constexpr int kCols = TOK ? 128 : N;
+        const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
         for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
             const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
             float acc[kCols];
@@ -431,7 +464,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
             const float *ws = a.w_scale + (static_cast<int64_t>(tile.expert) * a.w_blocks) * a.G;
             if constexpr (TOK) {
-                const int block = tile.w0 / kGroup + half;
+                const int block = (tile.w0 + part * kCols) / kGroup;
                 const bool columns = block < a.w_blocks;
                 ws += static_cast<int64_t>(columns ? block : 0) * a.G;
                 bool mine = row < tile.rows;
@@ -455,31 +488,29 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                         break;
                     }
                     tmem_fence_after();
-                    uint32_t d[2][16];
-                    tmem_load16(tmem_row + b * N, d[0]);
-                    tmem_wait16(d[0]);
 #pragma unroll
-                    for (int c = 0; c < kCols / 16; ++c) {
-                        if (c + 1 < kCols / 16) tmem_load16(tmem_row + b * N + (c + 1) * 16, d[(c + 1) & 1]);
-#pragma unroll
-                        for (int i = 0; i < 16; i += 2) fma_pair(acc[c * 16 + i], acc[c * 16 + i + 1], d[c & 1][i], d[c & 1][i + 1], s, s);
-                        if (c + 1 < kCols / 16) tmem_wait16(d[(c + 1) & 1]);
-                        if (c + 2 == kCols / 16) {
+                    for (int c = 0; c < kCols; c += 16) {
+                        uint32_t d[16];
+                        tmem_load16(tmem_row + b * N + c, d);
+                        tmem_wait16(d);
+                        if (c + 16 == kCols) {
                             tmem_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive(acc_empty + 8 * b);
                         }
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) fma_pair(acc[c + i], acc[c + i + 1], d[i], d[i + 1], s, s);
                     }
                 }
                 if (!ok) break;
-                const int64_t c0 = tile.w0 + half * 128;
+                const int64_t c0 = tile.w0 + part * kCols;
                 if (mine && columns) {
-                    const int valid = static_cast<int>(min(static_cast<int64_t>(128), a.M - c0));
+                    const int valid = static_cast<int>(min(static_cast<int64_t>(kCols), a.M - c0));
                     const int64_t at = (tile.row0 + row) * a.M + c0;
                     if (a.out_bf16) {
                         __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.y) + at;
 #pragma unroll
-                        for (int i = 0; i < 128; i += 8) {
+                        for (int i = 0; i < kCols; i += 8) {
                             if (a.vector && i + 8 <= valid) {
                                 *reinterpret_cast<uint4 *>(out + i) = make_uint4(bf16_pair(acc[i], acc[i + 1]), bf16_pair(acc[i + 2], acc[i + 3]),
                                                                                  bf16_pair(acc[i + 4], acc[i + 5]), bf16_pair(acc[i + 6], acc[i + 7]));
@@ -492,7 +523,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     } else {
                         float *out = static_cast<float *>(a.y) + at;
 #pragma unroll
-                        for (int i = 0; i < 128; i += 4) {
+                        for (int i = 0; i < kCols; i += 4) {
                             if (a.vector && i + 4 <= valid) {
                                 *reinterpret_cast<float4 *>(out + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
                             } else {
@@ -508,7 +539,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 // the scales of the tile's tokens: lane l looks after columns l, l + 32, ...; a group's products with the weights'
                 // scale pass through shared memory, a copy per warp
                 constexpr int kOwn = (N + 31) / 32;
-                float *scales = reinterpret_cast<float *>(smem + L::kScales) + (warp - 2) * 2 * N;
+                float *scales = reinterpret_cast<float *>(smem + L::kScales) + (warp - L::kFirst) * 2 * N;
                 const float *xs[kOwn];
                 uint32_t bad[kOwn];                // columns whose row of x does not exist: not written
                 float sx[kOwn];
@@ -591,7 +622,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     if constexpr (!GROUPED && !TOK) {
         if (splits > 1) {
             cluster_sync();
-            if (warp >= 2) {
+            if (warp >= L::kFirst) {
                 const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t_first);
                 const int row = (warp & 3) * 32 + lane;
                 const int64_t m = tile.w0 + row;
@@ -612,7 +643,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     __syncthreads();
     if (warp == 1) {
         tmem_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kColumns) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kTmemColumns) : "memory");
     }
 }
 
@@ -662,7 +693,7 @@ int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_r
     CUtensorMap wmap, xmap;
     int rc = encode(&wmap, W, K, args.M, experts, L::kWRowsPerTile);
     if (rc) return rc;
-    rc = encode(&xmap, x, K, x_rows, 0, GROUPED ? 1 : L::kRowsPerTile);
+    rc = encode(&xmap, x, K, x_rows, 0, L::kRowsPerTile);
     if (rc) return rc;
     auto *kernel = fp8_matmul_kernel<N, TOK, GROUPED>;
     static bool prepared[32];                // (per device; as in prepare_kernel, and all of the cache as shared memory)
@@ -810,6 +841,7 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
     a.out_bf16 = y_type == BITCOS_BF16;
     a.vector = M % (a.out_bf16 ? 8 : 4) == 0;
     a.splits = 1;
+    a.x = x;
     a.group_expert = group_expert;
     a.group_begin = group_begin;
     a.n_groups = n_groups_device;
@@ -830,7 +862,6 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
     if (mean <= 8) return launch_fp8<16, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     if (mean <= 16) return launch_fp8<32, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     if (mean <= 32) return launch_fp8<64, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
-    if (mean <= 64) return launch_fp8<128, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     a.w_tiles = static_cast<int>((M + 255) / 256);
     return launch_fp8<256, true, true>(W, x, K, n_experts, n_xrows, a, sms, stream);
 }
