@@ -107,6 +107,9 @@ constexpr int kARows = 128;               // rows of the A operand
 constexpr uint32_t kABytes = kARows * kGroup;
 constexpr int kMaxGroups = BITCOS_GROUP_EXPERTS_MAX;
 constexpr int kMaxSplits = 8;             // portable cluster size
+// Registers per thread, tokens first: what the block is launched with (checked before the first launch), and what the warps in
+// front and the promoters split it into.
+constexpr int kLaunchRegisters = 168, kFrontRegisters = 88, kPromoterRegisters = 208;
 
 struct Fp8Args {
     const float *w_scale;       // [experts][w_blocks][G]
@@ -139,17 +142,18 @@ struct Layout {
     static constexpr uint32_t kBBytes = N * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = TOK ? 4 : N <= 32 ? 5 : N == 64 ? 4 : 3;
-    static constexpr int kPromoters = TOK ? 16 : 4;     // warps
-    static constexpr int kFirst = GROUPED ? 4 : 2;      // the first of them (in front: TMA, tensor cores, two for gathered rows)
+    static constexpr int kParts = TOK ? 2 : 1;          // of the accumulator's columns, one for every four promoter warps
+    static constexpr int kColumns = N / kParts;         // per promoter thread
+    static constexpr int kPromoters = 4 * kParts;       // warps
+    static constexpr int kFirst = GROUPED || TOK ? 4 : 2;      // the first of them (in front: TMA, tensor cores, two for gathered rows)
     static constexpr int kThreads = (kFirst + kPromoters) * 32;
-    static constexpr int kColumns = TOK ? N / 4 : N;    // of the accumulator per promoter thread
     static constexpr int kRowsPerTile = TOK ? kARows : N;
     static constexpr int kWRowsPerTile = TOK ? N : kARows;
     static constexpr uint32_t kTmemColumns = 2 * N < 32 ? 32 : 2 * N;
     // byte offsets behind the stages
     static constexpr uint32_t kBars = kStages * kStageBytes;
-    static constexpr uint32_t kTmem = kBars + (2 * kStages + 4) * 8;
-    static constexpr uint32_t kScales = (kTmem + 16 + 15) / 16 * 16;
+    static constexpr uint32_t kTmem = kBars + (2 * kStages + 5) * 8;
+    static constexpr uint32_t kScales = (kTmem + 4 + 15) / 16 * 16;
     static constexpr uint32_t kPrefix = kScales + (TOK ? 0 : kPromoters * 2 * N * 4);
     static constexpr uint32_t kTotal = kPrefix + (GROUPED ? (kMaxGroups + 1) * 8 : 0);
     static constexpr uint32_t kDynamic = kTotal + 1024;  // (the stages start on a 1024-byte boundary)
@@ -206,8 +210,38 @@ __device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
                  :
                  : "memory");
 }
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                   "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                   "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :
+                 : "memory");
+}
+// One lane of a converged warp, the same one every time.  (Known to the compiler as one: the operands of tcgen05 and TMA instructions are
+// uniform registers, and behind a plain `lane == 0` every such instruction is wrapped in a loop over the lanes that may differ.)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+// A bounded wait.  (No call in it: with one, ptxas keeps every role to the registers that the block is launched with.)
+__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity) { return mbar_try(bar, parity) || mbar_wait_limited(bar, parity, kWaitLimitNs); }
 // A bounded wait by a whole warp, which goes on or gives up as one (what follows are instructions of whole warps).
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(kFull, mbar_wait(bar, parity)); }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(kFull, wait_here(bar, parity)); }
 // a += d * s, two at a time
 __device__ __forceinline__ void fma_pair(float &a0, float &a1, uint32_t d0, uint32_t d1, float s0, float s1) {
     asm("{\n\t.reg .b64 a, d, s;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 d, {%2, %3};\n\tmov.b64 s, {%4, %5};\n\t"
@@ -280,6 +314,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     uint8_t *smem = smem_raw + (1024u - (raw & 1023u)) % 1024u;
     const uint32_t base = smem_addr(smem);
     const uint32_t full = base + L::kBars, empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
+    const uint32_t drained = acc_empty + 16;
     int64_t *prefix = reinterpret_cast<int64_t *>(smem + L::kPrefix);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int splits = GROUPED || TOK ? 1 : a.splits;
@@ -287,7 +322,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     const int rank = splits > 1 ? static_cast<int>(cluster_rank()) : 0;
     const int k0 = static_cast<int>(static_cast<int64_t>(a.G) * rank / splits), k1 = static_cast<int>(static_cast<int64_t>(a.G) * (rank + 1) / splits);
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0 && elect_one()) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(full + 8 * s, gather ? 3 : 1);
             mbar_init(empty + 8 * s, 1);
@@ -296,6 +331,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             mbar_init(acc_full + 8 * b, 1);
             mbar_init(acc_empty + 8 * b, L::kPromoters);
         }
+        mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if constexpr (!GROUPED) {
             // the first weights are on their way before the kernel in front of this one has finished: they are nobody's output
@@ -358,101 +394,113 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     bool ok = true;
     uint32_t it = 0;                       // groups of 128 so far, over all tiles
 
-    if (warp == 0) {
-        // ---- producer
-        for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-            const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
-            for (int kb = k0; ok && kb < k1; ++kb, ++it) {
-                const uint32_t s = it % kStages;
-                const uint32_t stage = base + s * L::kStageBytes, bar = full + 8 * s;
-                const uint32_t w_dst = stage + (TOK ? kABytes : 0), x_dst = stage + (TOK ? 0 : kABytes);
-                if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
-                    ok = false;
-                    break;
-                }
-                const bool sent = !GROUPED && it < kStages && t == t_first;       // (announced and the weights sent above)
-                if (lane == 0) {
-                    if (!sent) {
-                        mbar_expect_tx(bar, gather ? L::kStageBytes - kXBytes : L::kStageBytes);
-                        tma_3d(w_dst, &wmap, kb * kGroup, tile.w0, tile.expert, bar);
-                    }
-                    if (!gather) tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), bar);
-                }
-            }
-        }
-        // no copy may outlive the block
-        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) ok &= mbar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
-    } else if (warp == 1) {
-        // ---- tensor cores: one lane
-        if (lane == 0) {
-            constexpr uint32_t idesc = instruction_desc(N);
-            for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-                for (int kb = k0; kb < k1; ++kb, ++it) {
-                    const uint32_t s = it % kStages, b = it & 1;
-                    if (it >= 2 && !mbar_wait(acc_empty + 8 * b, (it / 2 - 1) & 1)) {
-                        ok = false;
-                        break;
-                    }
-                    if (!mbar_wait(full + 8 * s, (it / kStages) & 1)) {
-                        ok = false;
-                        break;
-                    }
-                    tmem_fence_after();
-                    const uint64_t da = matrix_desc(base + s * L::kStageBytes), db = matrix_desc(base + s * L::kStageBytes + kABytes);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_e4m3(tmem + b * N, da + 2 * k, db + 2 * k, idesc, k > 0);
-                    mma_commit(empty + 8 * s);
-                    mma_commit(acc_full + 8 * b);
-                }
-            }
-            // nothing may be in flight when the tensor memory goes
-            for (uint32_t i = it > 2 ? it - 2 : 0; i < it; ++i) ok &= mbar_wait(acc_full + 8 * (i & 1), (i / 2) & 1);
-        }
-        __syncwarp();
-    } else if (GROUPED && warp < L::kFirst) {
-        // ---- rows of routed pairs: two warps, eight lanes per row of 128 bytes, 16 bytes each, put where the 128-byte swizzle has them
-        if (gather) {
-            constexpr int kOwn = L::kRowsPerTile / 8, kLag = kStages - 2;
-            const int p = threadIdx.x - 64, r0 = p >> 3, chunk = p & 7;
-            const uint32_t x_off = (TOK ? 0 : kABytes) + r0 * kGroup + ((chunk ^ (r0 & 7)) << 4);
-            const uint8_t *x = a.x + chunk * 16;
-            const int64_t K = static_cast<int64_t>(a.G) * kGroup;
-            // a stage is handed on when its copies have landed, kLag stages later
-            const auto hand_on = [&](uint32_t i) {
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(full + 8 * (i % kStages));
-            };
+    // Tokens first: a promoter holds 128 sums and 64 columns on their way; what it takes over 168 registers the four warps in
+    // front give.  (In the two branches themselves: where they meet, the smaller number holds.)
+    static_assert(!TOK || 128 * kFrontRegisters + L::kPromoters * 32 * kPromoterRegisters == L::kThreads * kLaunchRegisters, "the block's registers");
+    if (warp < L::kFirst) {
+        if (TOK) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFrontRegisters));
+        if (warp == 0) {
+            // ---- producer
             for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
                 const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
-                // what is not a row of the tile, or no row of x, reads row 0 and is dropped later
-                int src[kOwn];
-#pragma unroll
-                for (int j = 0; j < kOwn; ++j) {
-                    const int i = r0 + 8 * j;
-                    const int r = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : 0;
-                    src[j] = r >= 0 && r < a.n_xrows ? r : 0;
-                }
-                for (int kb = k0; kb < k1; ++kb, ++it) {
-                    const uint32_t s = it % kStages, dst = base + s * L::kStageBytes + x_off;
+                for (int kb = k0; ok && kb < k1; ++kb, ++it) {
+                    const uint32_t s = it % kStages;
+                    const uint32_t stage = base + s * L::kStageBytes, bar = full + 8 * s;
+                    const uint32_t w_dst = stage + (TOK ? kABytes : 0), x_dst = stage + (TOK ? 0 : kABytes);
                     if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
                         ok = false;
                         break;
                     }
-#pragma unroll
-                    for (int j = 0; j < kOwn; ++j) copy16(dst + j * 8 * kGroup, x + src[j] * K + kb * kGroup);
-                    asm volatile("cp.async.commit_group;" ::: "memory");
-                    if (it >= kLag) {
-                        asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-                        hand_on(it - kLag);
+                    const bool sent = !GROUPED && it < kStages && t == t_first;       // (announced and the weights sent above)
+                    if (elect_one()) {
+                        if (!sent) {
+                            mbar_expect_tx(bar, gather ? L::kStageBytes - kXBytes : L::kStageBytes);
+                            tma_3d(w_dst, &wmap, kb * kGroup, tile.w0, tile.expert, bar);
+                        }
+                        if (!gather) tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), bar);
                     }
+                    __syncwarp();
                 }
             }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            for (uint32_t i = it > kLag ? it - kLag : 0; i < it; ++i) hand_on(i);
+            // no copy may outlive the block
+            for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) ok &= wait_here(full + 8 * (i % kStages), (i / kStages) & 1);
+        } else if (warp == 1) {
+            // ---- tensor cores: the warp waits, one lane issues
+            constexpr uint32_t idesc = instruction_desc(N);
+            for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
+                for (int kb = k0; kb < k1; ++kb, ++it) {
+                    const uint32_t s = it % kStages, b = it & 1;
+                    // (both barriers are asked before either answer is looked at: an answer takes about 200 clocks here, and
+                    // this warp's turn has to stay below the 512 clocks of its products)
+                    const uint32_t have = mbar_try(full + 8 * s, (it / kStages) & 1);
+                    const uint32_t room = it < 2 || mbar_try(acc_empty + 8 * b, (it / 2 - 1) & 1);
+                    if (!__all_sync(kFull, have & room)) {
+                        if ((it >= 2 && !warp_wait(acc_empty + 8 * b, (it / 2 - 1) & 1)) || !warp_wait(full + 8 * s, (it / kStages) & 1)) {
+                            ok = false;
+                            break;
+                        }
+                    }
+                    tmem_fence_after();
+                    if (elect_one()) {
+                        const uint64_t da = matrix_desc(base + s * L::kStageBytes), db = matrix_desc(base + s * L::kStageBytes + kABytes);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mma_e4m3(tmem + b * N, da + 2 * k, db + 2 * k, idesc, k > 0);
+                        mma_commit(acc_full + 8 * b);
+                        mma_commit(empty + 8 * s);
+                    }
+                    __syncwarp();
+                }
+            }
+            // nothing may be in flight when the tensor memory goes
+            if (elect_one()) mma_commit(drained);
+            __syncwarp();
+            ok &= warp_wait(drained, 0);
+        } else if (L::kFirst == 4 && warp < L::kFirst) {
+            // ---- rows of routed pairs: two warps, eight lanes per row of 128 bytes, 16 bytes each, put where the 128-byte swizzle has them
+            if (gather) {
+                constexpr int kOwn = L::kRowsPerTile / 8, kLag = kStages - 2;
+                const int p = threadIdx.x - 64, r0 = p >> 3, chunk = p & 7;
+                const uint32_t x_off = (TOK ? 0 : kABytes) + r0 * kGroup + ((chunk ^ (r0 & 7)) << 4);
+                const uint8_t *x = a.x + chunk * 16;
+                const int64_t K = static_cast<int64_t>(a.G) * kGroup;
+                // a stage is handed on when its copies have landed, kLag stages later
+                const auto hand_on = [&](uint32_t i) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(full + 8 * (i % kStages));
+                };
+                for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
+                    const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
+                    // what is not a row of the tile, or no row of x, reads row 0 and is dropped later
+                    int src[kOwn];
+#pragma unroll
+                    for (int j = 0; j < kOwn; ++j) {
+                        const int i = r0 + 8 * j;
+                        const int r = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : 0;
+                        src[j] = r >= 0 && r < a.n_xrows ? r : 0;
+                    }
+                    for (int kb = k0; kb < k1; ++kb, ++it) {
+                        const uint32_t s = it % kStages, dst = base + s * L::kStageBytes + x_off;
+                        if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
+                            ok = false;
+                            break;
+                        }
+#pragma unroll
+                        for (int j = 0; j < kOwn; ++j) copy16(dst + j * 8 * kGroup, x + src[j] * K + kb * kGroup);
+                        asm volatile("cp.async.commit_group;" ::: "memory");
+                        if (it >= kLag) {
+                            asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+                            hand_on(it - kLag);
+                        }
+                    }
+                }
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                for (uint32_t i = it > kLag ? it - kLag : 0; i < it; ++i) hand_on(i);
+            }
         }
     } else {
         // ---- promoters: warp w of four reads lanes 32 (w % 4) .. + 31 of the accumulators
+        if (TOK) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPromoterRegisters));
         constexpr int kCols = L::kColumns;
         const int quarter = warp & 3, part = TOK ? (warp - L::kFirst) >> 2 : 0;
         const int row = quarter * 32 + lane;       // of A
@@ -488,18 +536,22 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                         break;
                     }
                     tmem_fence_after();
+                    // 64 columns at a time: a load's latency is paid twice per group
 #pragma unroll
-                    for (int c = 0; c < kCols; c += 16) {
-                        uint32_t d[16];
-                        tmem_load16(tmem_row + b * N + c, d);
-                        tmem_wait16(d);
-                        if (c + 16 == kCols) {
+                    for (int c = 0; c < kCols; c += 64) {
+                        uint32_t d[2][32];
+                        tmem_load32(tmem_row + b * N + c, d[0]);
+                        tmem_load32(tmem_row + b * N + c + 32, d[1]);
+                        tmem_wait32(d[0]);
+                        tmem_wait32(d[1]);
+                        if (c + 64 == kCols) {
                             tmem_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive(acc_empty + 8 * b);
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) fma_pair(acc[c + i], acc[c + i + 1], d[i], d[i + 1], s, s);
+                        for (int i = 0; i < 64; i += 2)
+                            fma_pair(acc[c + i], acc[c + i + 1], d[i / 32][i % 32], d[i / 32][i % 32 + 1], s, s);
                     }
                 }
                 if (!ok) break;
@@ -701,6 +753,15 @@ int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_r
     rc = check_cuda(cudaGetDevice(&dev));
     if (rc) return rc;
     if (dev >= 32 || !prepared[dev]) {
+        if (TOK) {
+            cudaFuncAttributes attributes{};
+            rc = check_cuda(cudaFuncGetAttributes(&attributes, kernel));
+            if (rc) return rc;
+            if (attributes.numRegs != kLaunchRegisters) {          // (the split would wait for registers that are not there)
+                g_last_cuda_error = cudaErrorInvalidDeviceFunction;
+                return BITCOS_ERR_CUDA;
+            }
+        }
         rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kDynamic)));
         if (rc == BITCOS_OK)
             rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
