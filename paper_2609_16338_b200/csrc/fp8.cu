@@ -137,11 +137,14 @@ struct Tile {
     int expert;
 };
 
-template <int N, bool TOK, bool GROUPED>
+// PAIR (tokens first, dense): two blocks of a cluster multiply as one, 256 tokens by 256 weight rows; each loads its own 128
+// tokens and half of the weight rows.
+template <int N, bool TOK, bool GROUPED, bool PAIR = false>
 struct Layout {
-    static constexpr uint32_t kBBytes = N * kGroup;
+    static constexpr int kBRows = PAIR ? N / 2 : N;     // of the B operand in this block's shared memory
+    static constexpr uint32_t kBBytes = kBRows * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = TOK ? 4 : N <= 32 ? 5 : N == 64 ? 4 : 3;
+    static constexpr int kStages = PAIR ? 6 : TOK ? 4 : N <= 32 ? 5 : N == 64 ? 4 : 3;
     static constexpr int kParts = TOK ? 2 : 1;          // of the accumulator's columns, one for every four promoter warps
     static constexpr int kColumns = N / kParts;         // per promoter thread
     static constexpr int kPromoters = 4 * kParts;       // warps
@@ -169,6 +172,18 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int
                  "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
                  : "memory");
 }
+// The same for a block of a pair, whose copies are counted by a barrier of the first block (an address in the cluster).
+__device__ __forceinline__ void tma_2d_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(map), "r"(c0), "r"(c1), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_3d_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+                 : "memory");
+}
+
 // 16 bytes from anywhere in global memory, asynchronously (the rows of routed pairs: one copy of a whole row's 128 bytes
 // by tile::gather4 costs the TMA unit about 25 clocks, 3300 a stage of 128 rows).
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
@@ -179,18 +194,31 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
 __device__ __forceinline__ uint64_t matrix_desc(uint32_t addr) {
     return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-// Instruction descriptor: e4m3 x e4m3 -> fp32, M = 128, N as given.
-__host__ __device__ constexpr uint32_t instruction_desc(int n) {
-    return (1u << 4) | (static_cast<uint32_t>(n / 8) << 17) | (static_cast<uint32_t>(kARows / 16) << 24);
+// Instruction descriptor: e4m3 x e4m3 -> fp32, M rows of A and N of B.
+__host__ __device__ constexpr uint32_t instruction_desc(int m, int n) {
+    return (1u << 4) | (static_cast<uint32_t>(n / 8) << 17) | (static_cast<uint32_t>(m / 16) << 24);
 }
+template <bool PAIR>
 __device__ __forceinline__ void mma_e4m3(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add)
-        : "memory");
+    if constexpr (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add)
+            : "memory");
 }
+// An arrival when all products so far are done (PAIR: at this barrier of both blocks, or with ALONE of this one).
+template <bool PAIR, bool ALONE = false>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (PAIR && ALONE) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    else if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(static_cast<uint16_t>(3))
+                     : "memory");
+    else asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -262,6 +290,17 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
     return r;
 }
+// The address in the cluster of another block's shared memory.
+__device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+// (Without .release.cluster: that waits for all of the thread's memory traffic, 1000 clocks a time, and what the arrival stands for are
+// reads of tensor memory that tcgen05.wait::ld has seen done and the tcgen05 fence orders.)
+__device__ __forceinline__ void cluster_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&p);
@@ -270,9 +309,9 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 // Where tile t lies.  Dense: bands of 16 tiles along the tokens, inside a band the tokens vary fastest, so that the tiles
 // that run at the same time share rows and weights in L2.  Grouped: the group by bisection in the running tile counts; inside a group
 // the tokens vary fastest (the tiles of one stretch of weights run side by side).
-template <int N, bool TOK, bool GROUPED>
-__device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefix, int n_groups, int64_t t) {
-    using L = Layout<N, TOK, GROUPED>;
+template <int N, bool TOK, bool GROUPED, bool PAIR>
+__device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefix, int n_groups, int64_t t, int rank) {
+    using L = Layout<N, TOK, GROUPED, PAIR>;
     Tile r;
     if constexpr (!GROUPED) {
         constexpr int kBand = 16;
@@ -281,8 +320,8 @@ __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefi
         const int wide = min(kBand, a.row_tiles - band * kBand);
         const int in = static_cast<int>(t - band * per_band);
         const int w = in / wide, row_tile = band * kBand + in - w * wide;
-        r.row0 = static_cast<int64_t>(row_tile) * L::kRowsPerTile;
-        r.rows = static_cast<int>(min(static_cast<int64_t>(L::kRowsPerTile), a.rows - r.row0));
+        r.row0 = (static_cast<int64_t>(row_tile) * (PAIR ? 2 : 1) + (PAIR ? rank : 0)) * L::kRowsPerTile;
+        r.rows = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(L::kRowsPerTile), a.rows - r.row0)));
         r.w0 = w * L::kWRowsPerTile;
         r.expert = 0;
     } else {
@@ -304,10 +343,10 @@ __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefi
     return r;
 }
 
-template <int N, bool TOK, bool GROUPED>
-__global__ void __launch_bounds__(Layout<N, TOK, GROUPED>::kThreads, TOK ? 1 : 2)
+template <int N, bool TOK, bool GROUPED, bool PAIR>
+__global__ void __launch_bounds__(Layout<N, TOK, GROUPED, PAIR>::kThreads, TOK ? 1 : 2)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ Fp8Args a) {
-    using L = Layout<N, TOK, GROUPED>;
+    using L = Layout<N, TOK, GROUPED, PAIR>;
     constexpr int kStages = L::kStages;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_addr(smem_raw);
@@ -319,8 +358,28 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int splits = GROUPED || TOK ? 1 : a.splits;
     const bool gather = GROUPED && a.pair_xrow != nullptr;
-    const int rank = splits > 1 ? static_cast<int>(cluster_rank()) : 0;
-    const int k0 = static_cast<int>(static_cast<int64_t>(a.G) * rank / splits), k1 = static_cast<int>(static_cast<int64_t>(a.G) * (rank + 1) / splits);
+    const int rank = PAIR || splits > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const int k_rank = PAIR ? 0 : rank;
+    const int k0 = static_cast<int>(static_cast<int64_t>(a.G) * k_rank / splits), k1 = static_cast<int>(static_cast<int64_t>(a.G) * (k_rank + 1) / splits);
+    const int64_t per_tile = PAIR ? 2 : splits;              // blocks that work on one tile
+    const int64_t t_first = blockIdx.x / per_tile, t_step = gridDim.x / per_tile;
+    // PAIR: the barriers that the tensor cores wait on are the first block's
+    const uint32_t lead_full = PAIR ? cluster_address(full, 0) : full, lead_acc_empty = PAIR ? cluster_address(acc_empty, 0) : acc_empty;
+    const auto send_weights = [&](uint32_t stage, const Tile &t, int kb, uint32_t bar) {
+        const uint32_t dst = base + stage * L::kStageBytes + (TOK ? kABytes : 0);
+        if constexpr (PAIR) tma_3d_pair(dst, &wmap, kb * kGroup, t.w0 + rank * L::kBRows, t.expert, bar);
+        else tma_3d(dst, &wmap, kb * kGroup, t.w0, t.expert, bar);
+    };
+    // the first weights are on their way before the kernel in front of this one has finished: they are nobody's output
+    const auto send_first = [&]() {
+        if (t_first < static_cast<int64_t>(a.row_tiles) * a.w_tiles) {
+            const Tile t = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, 0, t_first, rank);
+            for (int i = 0; i < kStages && k0 + i < k1; ++i) {
+                if (!PAIR || rank == 0) mbar_expect_tx(full + 8 * i, (PAIR ? 2 : 1) * L::kStageBytes);
+                send_weights(i, t, k0 + i, lead_full + 8 * i);
+            }
+        }
+    };
 
     if (warp == 0 && elect_one()) {
         for (int s = 0; s < kStages; ++s) {
@@ -329,33 +388,31 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full + 8 * b, 1);
-            mbar_init(acc_empty + 8 * b, L::kPromoters);
+            mbar_init(acc_empty + 8 * b, (PAIR ? 2 : 1) * L::kPromoters);
         }
         mbar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        if constexpr (!GROUPED) {
-            // the first weights are on their way before the kernel in front of this one has finished: they are nobody's output
-            if (blockIdx.x / splits < static_cast<int64_t>(a.row_tiles) * a.w_tiles) {
-                const Tile t = find_tile<N, TOK, GROUPED>(a, prefix, 0, blockIdx.x / splits);
-                for (int i = 0; i < kStages && k0 + i < k1; ++i) {
-                    const uint32_t dst = base + i * L::kStageBytes + (TOK ? kABytes : 0);
-                    mbar_expect_tx(full + 8 * i, L::kStageBytes);
-                    tma_3d(dst, &wmap, (k0 + i) * kGroup, t.w0, 0, full + 8 * i);
-                }
-            }
-        }
+        if (!GROUPED && !PAIR) send_first();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kTmem), "n"(L::kTmemColumns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kTmem), "n"(L::kTmemColumns) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kTmem), "n"(L::kTmemColumns) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
         tmem_fence_before();
     }
-    __syncthreads();
+    if constexpr (PAIR) cluster_sync();                      // (the other block's barriers are there, and its tensor memory)
+    else __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + L::kTmem);
     // The next kernel's blocks may start only once every block of this one holds its tensor memory: a block of the next kernel that
     // got it first would keep it until this kernel is done.
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (PAIR && warp == 0 && elect_one()) send_first();
+    __syncwarp();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     int n_groups = 0;
@@ -389,7 +446,6 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         __syncthreads();
         n_tiles = prefix[n_groups];
     }
-    const int64_t t_first = blockIdx.x / splits, t_step = gridDim.x / splits;
     constexpr uint32_t kXBytes = TOK ? kABytes : L::kBBytes;
     bool ok = true;
     uint32_t it = 0;                       // groups of 128 so far, over all tiles
@@ -402,11 +458,10 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         if (warp == 0) {
             // ---- producer
             for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-                const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
+                const Tile tile = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, n_groups, t, rank);
                 for (int kb = k0; ok && kb < k1; ++kb, ++it) {
                     const uint32_t s = it % kStages;
-                    const uint32_t stage = base + s * L::kStageBytes, bar = full + 8 * s;
-                    const uint32_t w_dst = stage + (TOK ? kABytes : 0), x_dst = stage + (TOK ? 0 : kABytes);
+                    const uint32_t x_dst = base + s * L::kStageBytes + (TOK ? 0 : kABytes);
                     if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
                         ok = false;
                         break;
@@ -414,20 +469,23 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     const bool sent = !GROUPED && it < kStages && t == t_first;       // (announced and the weights sent above)
                     if (elect_one()) {
                         if (!sent) {
-                            mbar_expect_tx(bar, gather ? L::kStageBytes - kXBytes : L::kStageBytes);
-                            tma_3d(w_dst, &wmap, kb * kGroup, tile.w0, tile.expert, bar);
+                            if (!PAIR || rank == 0) mbar_expect_tx(full + 8 * s, gather ? L::kStageBytes - kXBytes : (PAIR ? 2 : 1) * L::kStageBytes);
+                            send_weights(s, tile, kb, lead_full + 8 * s);
                         }
-                        if (!gather) tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), bar);
+                        if constexpr (PAIR) tma_2d_pair(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), lead_full + 8 * s);
+                        else if (!gather) tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), full + 8 * s);
                     }
                     __syncwarp();
                 }
             }
-            // no copy may outlive the block
-            for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) ok &= wait_here(full + 8 * (i % kStages), (i / kStages) & 1);
+            // no copy may outlive the block, and (PAIR) no arrival from the other block's products: every stage has been read
+            for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
+                ok = warp_wait((PAIR ? empty : full) + 8 * (i % kStages), (i / kStages) & 1);
         } else if (warp == 1) {
             // ---- tensor cores: the warp waits, one lane issues
-            constexpr uint32_t idesc = instruction_desc(N);
-            for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
+            constexpr uint32_t idesc = instruction_desc(PAIR ? 2 * kARows : kARows, N);
+            const bool issues = !PAIR || rank == 0;
+            for (int64_t t = t_first; issues && ok && t < n_tiles; t += t_step) {
                 for (int kb = k0; kb < k1; ++kb, ++it) {
                     const uint32_t s = it % kStages, b = it & 1;
                     // (both barriers are asked before either answer is looked at: an answer takes about 200 clocks here, and
@@ -444,17 +502,19 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     if (elect_one()) {
                         const uint64_t da = matrix_desc(base + s * L::kStageBytes), db = matrix_desc(base + s * L::kStageBytes + kABytes);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) mma_e4m3(tmem + b * N, da + 2 * k, db + 2 * k, idesc, k > 0);
-                        mma_commit(acc_full + 8 * b);
-                        mma_commit(empty + 8 * s);
+                        for (int k = 0; k < 4; ++k) mma_e4m3<PAIR>(tmem + b * N, da + 2 * k, db + 2 * k, idesc, k > 0);
+                        mma_commit<PAIR>(acc_full + 8 * b);
+                        mma_commit<PAIR>(empty + 8 * s);
                     }
                     __syncwarp();
                 }
             }
             // nothing may be in flight when the tensor memory goes
-            if (elect_one()) mma_commit(drained);
-            __syncwarp();
-            ok &= warp_wait(drained, 0);
+            if (issues) {
+                if (elect_one()) mma_commit<PAIR, true>(drained);
+                __syncwarp();
+                ok &= warp_wait(drained, 0);
+            }
         } else if (L::kFirst == 4 && warp < L::kFirst) {
             // ---- rows of routed pairs: two warps, eight lanes per row of 128 bytes, 16 bytes each, put where the 128-byte swizzle has them
             if (gather) {
@@ -470,7 +530,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     if (lane == 0) mbar_arrive(full + 8 * (i % kStages));
                 };
                 for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-                    const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
+                    const Tile tile = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, n_groups, t, rank);
                     // what is not a row of the tile, or no row of x, reads row 0 and is dropped later
                     int src[kOwn];
 #pragma unroll
@@ -506,7 +566,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         const int row = quarter * 32 + lane;       // of A
         const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
         for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-            const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t);
+            const Tile tile = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, n_groups, t, rank);
             float acc[kCols];
 #pragma unroll
             for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
@@ -523,35 +583,49 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     if (a.status) *a.status = 2u;
                 }
                 const float *xs = a.x_scale + (mine ? xr : 0) * a.G;
-                float sx = __ldg(xs + k0), sw = __ldg(ws + k0);
-                for (int kb = k0; kb < k1; ++kb, ++it) {
-                    const uint32_t b = it & 1;
-                    const float s = sx * sw;
-                    if (kb + 1 < k1) {
-                        sx = __ldg(xs + kb + 1);
-                        sw = __ldg(ws + kb + 1);
-                    }
-                    if (!warp_wait(acc_full + 8 * b, (it / 2) & 1)) {
-                        ok = false;
-                        break;
-                    }
+                // The columns pass 32 at a time through two buffers: while one is added, the other is on its way, across the groups
+                // too; the scales are asked for two groups ahead.
+                float scale = __ldg(xs + k0) * __ldg(ws + k0);
+                float sx = k0 + 1 < k1 ? __ldg(xs + k0 + 1) : 0.f, sw = k0 + 1 < k1 ? __ldg(ws + k0 + 1) : 0.f;
+                uint32_t d[2][32];
+                ok = warp_wait(acc_full + 8 * (it & 1), (it / 2) & 1);
+                if (ok) {
                     tmem_fence_after();
-                    // 64 columns at a time: a load's latency is paid twice per group
+                    tmem_load32(tmem_row + (it & 1) * N, d[0]);
+                }
+                for (int kb = k0; ok && kb < k1; ++kb) {
+                    const uint32_t b = it & 1;
+                    const float s = scale;
+                    scale = sx * sw;
+                    if (kb + 2 < k1) {
+                        sx = __ldg(xs + kb + 2);
+                        sw = __ldg(ws + kb + 2);
+                    }
+                    ++it;
+                    uint32_t next = 1;
 #pragma unroll
-                    for (int c = 0; c < kCols; c += 64) {
-                        uint32_t d[2][32];
-                        tmem_load32(tmem_row + b * N + c, d[0]);
-                        tmem_load32(tmem_row + b * N + c + 32, d[1]);
-                        tmem_wait32(d[0]);
-                        tmem_wait32(d[1]);
-                        if (c + 64 == kCols) {
+                    for (int c = 0; c < kCols / 32; ++c) {
+                        tmem_wait32(d[c & 1]);
+                        if (c + 1 < kCols / 32) {
+                            tmem_load32(tmem_row + b * N + (c + 1) * 32, d[(c + 1) & 1]);
+                        } else {
                             tmem_fence_before();
                             __syncwarp();
-                            if (lane == 0) mbar_arrive(acc_empty + 8 * b);
+                            if (lane == 0) {
+                                if constexpr (PAIR) cluster_arrive(lead_acc_empty + 8 * b);
+                                else mbar_arrive(acc_empty + 8 * b);
+                            }
+                            if (kb + 1 < k1) next = mbar_try(acc_full + 8 * (it & 1), (it / 2) & 1);
                         }
 #pragma unroll
-                        for (int i = 0; i < 64; i += 2)
-                            fma_pair(acc[c + i], acc[c + i + 1], d[i / 32][i % 32], d[i / 32][i % 32 + 1], s, s);
+                        for (int i = 0; i < 32; i += 2) fma_pair(acc[c * 32 + i], acc[c * 32 + i + 1], d[c & 1][i], d[c & 1][i + 1], s, s);
+                    }
+                    if (kb + 1 < k1) {
+                        ok = __all_sync(kFull, next) || warp_wait(acc_full + 8 * (it & 1), (it / 2) & 1);
+                        if (ok) {
+                            tmem_fence_after();
+                            tmem_load32(tmem_row + (it & 1) * N, d[0]);
+                        }
                     }
                 }
                 if (!ok) break;
@@ -675,7 +749,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         if (splits > 1) {
             cluster_sync();
             if (warp >= L::kFirst) {
-                const Tile tile = find_tile<N, TOK, GROUPED>(a, prefix, n_groups, t_first);
+                const Tile tile = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, n_groups, t_first, rank);
                 const int row = (warp & 3) * 32 + lane;
                 const int64_t m = tile.w0 + row;
                 for (int n = rank; n < tile.rows; n += splits) {
@@ -692,10 +766,12 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
     }
     tmem_fence_before();
-    __syncthreads();
+    if constexpr (PAIR) cluster_sync();                      // (neither block goes while the other's copies or products may reach it)
+    else __syncthreads();
     if (warp == 1) {
         tmem_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kTmemColumns) : "memory");
+        if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kTmemColumns) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kTmemColumns) : "memory");
     }
 }
 
@@ -737,17 +813,17 @@ int encode(CUtensorMap *map, const void *data, int64_t K, int64_t rows, int expe
     return BITCOS_OK;
 }
 
-template <int N, bool TOK, bool GROUPED>
+template <int N, bool TOK, bool GROUPED, bool PAIR = false>
 int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_rows, const Fp8Args &args, int64_t blocks, cudaStream_t stream) {
-    using L = Layout<N, TOK, GROUPED>;
+    using L = Layout<N, TOK, GROUPED, PAIR>;
     static_assert(TOK || 2 * (L::kDynamic + 1024) <= 228 * 1024, "two blocks per multiprocessor");
     static_assert(L::kDynamic <= 227 * 1024, "shared memory of a block");
     CUtensorMap wmap, xmap;
-    int rc = encode(&wmap, W, K, args.M, experts, L::kWRowsPerTile);
+    int rc = encode(&wmap, W, K, args.M, experts, TOK ? L::kBRows : kARows);
     if (rc) return rc;
     rc = encode(&xmap, x, K, x_rows, 0, L::kRowsPerTile);
     if (rc) return rc;
-    auto *kernel = fp8_matmul_kernel<N, TOK, GROUPED>;
+    auto *kernel = fp8_matmul_kernel<N, TOK, GROUPED, PAIR>;
     static bool prepared[32];                // (per device; as in prepare_kernel, and all of the cache as shared memory)
     int dev = 0;
     rc = check_cuda(cudaGetDevice(&dev));
@@ -776,12 +852,13 @@ int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_r
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(args.splits);
+    const int cluster = PAIR ? 2 : args.splits;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = args.splits > 1 ? attr : attr + 1;
-    cfg.numAttrs = (args.splits > 1 ? 1 : 0) + ((env && env[0] == '0') ? 0 : 1);
+    cfg.attrs = cluster > 1 ? attr : attr + 1;
+    cfg.numAttrs = (cluster > 1 ? 1 : 0) + ((env && env[0] == '0') ? 0 : 1);
     void *pointers[] = {&wmap, &xmap, const_cast<Fp8Args *>(&args)};
     return check_cuda(cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(kernel), pointers));
 }
@@ -863,6 +940,13 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
     rc = multiprocessors(&sms);
     if (rc) return rc;
     const int64_t row_tiles = (rows + kARows - 1) / kARows, w_tiles = (M + 255) / 256;
+    const int64_t pairs = (rows + 2 * kARows - 1) / (2 * kARows);
+    if (rows > 128 && pairs * w_tiles >= sms / 4) {
+        if (pairs * w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
+        a.row_tiles = static_cast<int>(pairs);
+        a.w_tiles = static_cast<int>(w_tiles);
+        return launch_fp8<256, true, false, true>(W, x, K, 1, rows, a, 2 * std::min<int64_t>(pairs * w_tiles, sms / 2), stream);
+    }
     if (rows > 128 && row_tiles * w_tiles >= sms / 2) {
         if (row_tiles * w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
         a.row_tiles = static_cast<int>(row_tiles);
