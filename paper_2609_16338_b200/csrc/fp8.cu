@@ -139,25 +139,28 @@ struct Tile {
 
 // PAIR (tokens first, dense): two blocks of a cluster multiply as one, 256 tokens by 256 weight rows; each loads its own 128
 // tokens and half of the weight rows.
-template <int N, bool TOK, bool GROUPED, bool PAIR = false>
+template <int N, bool PAIR, bool GROUPED>
 struct Layout {
     static constexpr int kBRows = PAIR ? N / 2 : N;     // of the B operand in this block's shared memory
     static constexpr uint32_t kBBytes = kBRows * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = PAIR ? 6 : TOK ? 4 : N <= 32 ? 5 : N == 64 ? 4 : 3;
-    static constexpr int kParts = TOK ? 2 : 1;          // of the accumulator's columns, one for every four promoter warps
+    static constexpr int kStages = PAIR ? 5 : N <= 32 ? 5 : N == 64 ? 4 : 3;
+    static constexpr int kParts = PAIR ? 2 : 1;          // of the accumulator's columns, one for every four promoter warps
     static constexpr int kColumns = N / kParts;         // per promoter thread
     static constexpr int kPromoters = 4 * kParts;       // warps
-    static constexpr int kFirst = GROUPED || TOK ? 4 : 2;      // the first of them (in front: TMA, tensor cores, two for gathered rows)
+    static constexpr int kFirst = GROUPED || PAIR ? 4 : 2;      // the first of them (in front: TMA, tensor cores, two for gathered rows)
     static constexpr int kThreads = (kFirst + kPromoters) * 32;
-    static constexpr int kRowsPerTile = TOK ? kARows : N;
-    static constexpr int kWRowsPerTile = TOK ? N : kARows;
+    static constexpr int kRowsPerTile = PAIR ? kARows : N;              // tokens of a tile in this block
+    static constexpr int kTileRows = PAIR ? 2 * kRowsPerTile : kRowsPerTile;
+    static constexpr int kWRowsPerTile = PAIR ? N : kARows;
     static constexpr uint32_t kTmemColumns = 2 * N < 32 ? 32 : 2 * N;
     // byte offsets behind the stages
     static constexpr uint32_t kBars = kStages * kStageBytes;
     static constexpr uint32_t kTmem = kBars + (2 * kStages + 5) * 8;
     static constexpr uint32_t kScales = (kTmem + 4 + 15) / 16 * 16;
-    static constexpr uint32_t kPrefix = kScales + (TOK ? 0 : kPromoters * 2 * N * 4);
+    // PAIR: 32 rows of 128 bytes and 16 of padding per promoter warp, through which the outputs go to memory by whole lines
+    static constexpr uint32_t kOutPitch = 144, kOutBytes = 32 * kOutPitch;
+    static constexpr uint32_t kPrefix = kScales + (PAIR ? kPromoters * kOutBytes : kPromoters * 2 * N * 4);
     static constexpr uint32_t kTotal = kPrefix + (GROUPED ? (kMaxGroups + 1) * 8 : 0);
     static constexpr uint32_t kDynamic = kTotal + 1024;  // (the stages start on a 1024-byte boundary)
 };
@@ -296,8 +299,9 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
     return a;
 }
-// (Without .release.cluster: that waits for all of the thread's memory traffic, 1000 clocks a time, and what the arrival stands for are
-// reads of tensor memory that tcgen05.wait::ld has seen done and the tcgen05 fence orders.)
+// (Without .release.cluster: that waits for all of the thread's memory traffic, 1000 clocks a time, and what the arrival stands for
+// is done before it goes out and is nobody else's: reads of tensor memory that tcgen05.wait::ld has seen done, or copies that
+// cp.async.wait_group has seen land in this block's shared memory, where this multiprocessor's own tensor cores read them.)
 __device__ __forceinline__ void cluster_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -309,9 +313,9 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 // Where tile t lies.  Dense: bands of 16 tiles along the tokens, inside a band the tokens vary fastest, so that the tiles
 // that run at the same time share rows and weights in L2.  Grouped: the group by bisection in the running tile counts; inside a group
 // the tokens vary fastest (the tiles of one stretch of weights run side by side).
-template <int N, bool TOK, bool GROUPED, bool PAIR>
+template <int N, bool PAIR, bool GROUPED>
 __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefix, int n_groups, int64_t t, int rank) {
-    using L = Layout<N, TOK, GROUPED, PAIR>;
+    using L = Layout<N, PAIR, GROUPED>;
     Tile r;
     if constexpr (!GROUPED) {
         constexpr int kBand = 16;
@@ -320,7 +324,7 @@ __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefi
         const int wide = min(kBand, a.row_tiles - band * kBand);
         const int in = static_cast<int>(t - band * per_band);
         const int w = in / wide, row_tile = band * kBand + in - w * wide;
-        r.row0 = (static_cast<int64_t>(row_tile) * (PAIR ? 2 : 1) + (PAIR ? rank : 0)) * L::kRowsPerTile;
+        r.row0 = static_cast<int64_t>(row_tile) * L::kTileRows + (PAIR ? rank * L::kRowsPerTile : 0);
         r.rows = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(L::kRowsPerTile), a.rows - r.row0)));
         r.w0 = w * L::kWRowsPerTile;
         r.expert = 0;
@@ -332,21 +336,21 @@ __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefi
             else hi = mid;
         }
         const int begin = __ldg(a.group_begin + lo), end = __ldg(a.group_begin + lo + 1);
-        const int row_tiles = (end - begin + L::kRowsPerTile - 1) / L::kRowsPerTile;
+        const int row_tiles = (end - begin + L::kTileRows - 1) / L::kTileRows;
         const int in = static_cast<int>(t - prefix[lo]);
         const int w = in / row_tiles, row_tile = in - w * row_tiles;
-        r.row0 = begin + static_cast<int64_t>(row_tile) * L::kRowsPerTile;
-        r.rows = min(L::kRowsPerTile, static_cast<int>(end - r.row0));
+        r.row0 = begin + static_cast<int64_t>(row_tile) * L::kTileRows + (PAIR ? rank * L::kRowsPerTile : 0);
+        r.rows = max(0, min(L::kRowsPerTile, static_cast<int>(end - r.row0)));
         r.w0 = w * L::kWRowsPerTile;
         r.expert = __ldg(a.group_expert + lo);
     }
     return r;
 }
 
-template <int N, bool TOK, bool GROUPED, bool PAIR>
-__global__ void __launch_bounds__(Layout<N, TOK, GROUPED, PAIR>::kThreads, TOK ? 1 : 2)
+template <int N, bool PAIR, bool GROUPED>
+__global__ void __launch_bounds__(Layout<N, PAIR, GROUPED>::kThreads, PAIR ? 1 : 2)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ Fp8Args a) {
-    using L = Layout<N, TOK, GROUPED, PAIR>;
+    using L = Layout<N, PAIR, GROUPED>;
     constexpr int kStages = L::kStages;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_addr(smem_raw);
@@ -356,7 +360,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     const uint32_t drained = acc_empty + 16;
     int64_t *prefix = reinterpret_cast<int64_t *>(smem + L::kPrefix);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int splits = GROUPED || TOK ? 1 : a.splits;
+    const int splits = GROUPED || PAIR ? 1 : a.splits;
     const bool gather = GROUPED && a.pair_xrow != nullptr;
     const int rank = PAIR || splits > 1 ? static_cast<int>(cluster_rank()) : 0;
     const int k_rank = PAIR ? 0 : rank;
@@ -366,14 +370,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     // PAIR: the barriers that the tensor cores wait on are the first block's
     const uint32_t lead_full = PAIR ? cluster_address(full, 0) : full, lead_acc_empty = PAIR ? cluster_address(acc_empty, 0) : acc_empty;
     const auto send_weights = [&](uint32_t stage, const Tile &t, int kb, uint32_t bar) {
-        const uint32_t dst = base + stage * L::kStageBytes + (TOK ? kABytes : 0);
+        const uint32_t dst = base + stage * L::kStageBytes + (PAIR ? kABytes : 0);
         if constexpr (PAIR) tma_3d_pair(dst, &wmap, kb * kGroup, t.w0 + rank * L::kBRows, t.expert, bar);
         else tma_3d(dst, &wmap, kb * kGroup, t.w0, t.expert, bar);
     };
     // the first weights are on their way before the kernel in front of this one has finished: they are nobody's output
     const auto send_first = [&]() {
         if (t_first < static_cast<int64_t>(a.row_tiles) * a.w_tiles) {
-            const Tile t = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, 0, t_first, rank);
+            const Tile t = find_tile<N, PAIR, GROUPED>(a, prefix, 0, t_first, rank);
             for (int i = 0; i < kStages && k0 + i < k1; ++i) {
                 if (!PAIR || rank == 0) mbar_expect_tx(full + 8 * i, (PAIR ? 2 : 1) * L::kStageBytes);
                 send_weights(i, t, k0 + i, lead_full + 8 * i);
@@ -383,7 +387,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
 
     if (warp == 0 && elect_one()) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(full + 8 * s, gather ? 3 : 1);
+            mbar_init(full + 8 * s, gather ? (PAIR ? 5 : 3) : 1);
             mbar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -411,7 +415,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     // The next kernel's blocks may start only once every block of this one holds its tensor memory: a block of the next kernel that
     // got it first would keep it until this kernel is done.
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (PAIR && warp == 0 && elect_one()) send_first();
+    if (PAIR && !GROUPED && warp == 0 && elect_one()) send_first();
     __syncwarp();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
@@ -429,7 +433,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     if (end > begin) {
                         // a malformed group is skipped whole and marked (an empty one without a mark)
                         if (e >= 0 && e < a.n_experts && begin >= 0 && end <= a.rows)
-                            tiles = static_cast<int64_t>((end - begin + L::kRowsPerTile - 1) / L::kRowsPerTile) * a.w_tiles;
+                            tiles = static_cast<int64_t>((end - begin + L::kTileRows - 1) / L::kTileRows) * a.w_tiles;
                         else if (a.status && blockIdx.x == 0) *a.status = 2u;
                     }
                 }
@@ -446,22 +450,22 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         __syncthreads();
         n_tiles = prefix[n_groups];
     }
-    constexpr uint32_t kXBytes = TOK ? kABytes : L::kBBytes;
+    constexpr uint32_t kXBytes = PAIR ? kABytes : L::kBBytes;
     bool ok = true;
     uint32_t it = 0;                       // groups of 128 so far, over all tiles
 
     // Tokens first: a promoter holds 128 sums and 64 columns on their way; what it takes over 168 registers the four warps in
     // front give.  (In the two branches themselves: where they meet, the smaller number holds.)
-    static_assert(!TOK || 128 * kFrontRegisters + L::kPromoters * 32 * kPromoterRegisters == L::kThreads * kLaunchRegisters, "the block's registers");
+    static_assert(!PAIR || 128 * kFrontRegisters + L::kPromoters * 32 * kPromoterRegisters == L::kThreads * kLaunchRegisters, "the block's registers");
     if (warp < L::kFirst) {
-        if (TOK) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFrontRegisters));
+        if (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFrontRegisters));
         if (warp == 0) {
             // ---- producer
             for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-                const Tile tile = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, n_groups, t, rank);
+                const Tile tile = find_tile<N, PAIR, GROUPED>(a, prefix, n_groups, t, rank);
                 for (int kb = k0; ok && kb < k1; ++kb, ++it) {
                     const uint32_t s = it % kStages;
-                    const uint32_t x_dst = base + s * L::kStageBytes + (TOK ? 0 : kABytes);
+                    const uint32_t x_dst = base + s * L::kStageBytes + (PAIR ? 0 : kABytes);
                     if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
                         ok = false;
                         break;
@@ -469,11 +473,13 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     const bool sent = !GROUPED && it < kStages && t == t_first;       // (announced and the weights sent above)
                     if (elect_one()) {
                         if (!sent) {
-                            if (!PAIR || rank == 0) mbar_expect_tx(full + 8 * s, gather ? L::kStageBytes - kXBytes : (PAIR ? 2 : 1) * L::kStageBytes);
+                            if (!PAIR || rank == 0) mbar_expect_tx(full + 8 * s, (PAIR ? 2 : 1) * (gather ? L::kStageBytes - kXBytes : L::kStageBytes));
                             send_weights(s, tile, kb, lead_full + 8 * s);
                         }
-                        if constexpr (PAIR) tma_2d_pair(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), lead_full + 8 * s);
-                        else if (!gather) tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), full + 8 * s);
+                        if (!gather) {
+                            if constexpr (PAIR) tma_2d_pair(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), lead_full + 8 * s);
+                            else tma_2d(x_dst, &xmap, kb * kGroup, static_cast<int>(tile.row0), full + 8 * s);
+                        }
                     }
                     __syncwarp();
                 }
@@ -520,17 +526,20 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             if (gather) {
                 constexpr int kOwn = L::kRowsPerTile / 8, kLag = kStages - 2;
                 const int p = threadIdx.x - 64, r0 = p >> 3, chunk = p & 7;
-                const uint32_t x_off = (TOK ? 0 : kABytes) + r0 * kGroup + ((chunk ^ (r0 & 7)) << 4);
+                const uint32_t x_off = (PAIR ? 0 : kABytes) + r0 * kGroup + ((chunk ^ (r0 & 7)) << 4);
                 const uint8_t *x = a.x + chunk * 16;
                 const int64_t K = static_cast<int64_t>(a.G) * kGroup;
                 // a stage is handed on when its copies have landed, kLag stages later
                 const auto hand_on = [&](uint32_t i) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(full + 8 * (i % kStages));
+                    if (lane == 0) {
+                        if constexpr (PAIR) cluster_arrive(lead_full + 8 * (i % kStages));
+                        else mbar_arrive(full + 8 * (i % kStages));
+                    }
                 };
                 for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-                    const Tile tile = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, n_groups, t, rank);
+                    const Tile tile = find_tile<N, PAIR, GROUPED>(a, prefix, n_groups, t, rank);
                     // what is not a row of the tile, or no row of x, reads row 0 and is dropped later
                     int src[kOwn];
 #pragma unroll
@@ -560,18 +569,18 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
     } else {
         // ---- promoters: warp w of four reads lanes 32 (w % 4) .. + 31 of the accumulators
-        if (TOK) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPromoterRegisters));
+        if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPromoterRegisters));
         constexpr int kCols = L::kColumns;
-        const int quarter = warp & 3, part = TOK ? (warp - L::kFirst) >> 2 : 0;
+        const int quarter = warp & 3, part = PAIR ? (warp - L::kFirst) >> 2 : 0;
         const int row = quarter * 32 + lane;       // of A
         const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
         for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-            const Tile tile = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, n_groups, t, rank);
+            const Tile tile = find_tile<N, PAIR, GROUPED>(a, prefix, n_groups, t, rank);
             float acc[kCols];
 #pragma unroll
             for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
             const float *ws = a.w_scale + (static_cast<int64_t>(tile.expert) * a.w_blocks) * a.G;
-            if constexpr (TOK) {
+            if constexpr (PAIR) {
                 const int block = (tile.w0 + part * kCols) / kGroup;
                 const bool columns = block < a.w_blocks;
                 ws += static_cast<int64_t>(columns ? block : 0) * a.G;
@@ -630,34 +639,55 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 }
                 if (!ok) break;
                 const int64_t c0 = tile.w0 + part * kCols;
-                if (mine && columns) {
-                    const int valid = static_cast<int>(min(static_cast<int64_t>(kCols), a.M - c0));
-                    const int64_t at = (tile.row0 + row) * a.M + c0;
-                    if (a.out_bf16) {
-                        __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.y) + at;
+                // A thread has a row, memory wants lines: each warp turns its 32 rows round in shared memory, 128 bytes of a row
+                // at a time.  (Straight from the registers, 32 rows an instruction and half a sector each, a tile took 5 us.)
+                const uint32_t rows_mask = __ballot_sync(kFull, mine);
+                uint8_t *out = smem + L::kScales + (warp - L::kFirst) * L::kOutBytes;
+                const auto flush = [&](int from, int width) {           // columns from .. + width: 128 bytes
+                    __syncwarp();
+                    const int64_t first = tile.row0 + quarter * 32;
+                    const int left = static_cast<int>(min(static_cast<int64_t>(width), a.M - c0 - from)), size = 128 / width;
+                    if (a.vector) {
+                        const int at = (lane & 7) * (width / 8);
 #pragma unroll
-                        for (int i = 0; i < kCols; i += 8) {
-                            if (a.vector && i + 8 <= valid) {
-                                *reinterpret_cast<uint4 *>(out + i) = make_uint4(bf16_pair(acc[i], acc[i + 1]), bf16_pair(acc[i + 2], acc[i + 3]),
-                                                                                 bf16_pair(acc[i + 4], acc[i + 5]), bf16_pair(acc[i + 6], acc[i + 7]));
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    if (i + j < valid) out[i + j] = __float2bfloat16_rn(acc[i + j]);
-                            }
+                        for (int j = 0; j < 8; ++j) {
+                            const int r = (lane >> 3) + 4 * j;
+                            const uint4 v = *reinterpret_cast<const uint4 *>(out + r * L::kOutPitch + (lane & 7) * 16);
+                            if (((rows_mask >> r) & 1u) && at < left)
+                                *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.y) + ((first + r) * a.M + c0 + from + at) * size) = v;
                         }
                     } else {
-                        float *out = static_cast<float *>(a.y) + at;
+                        for (int r = 0; r < 32; ++r)
+                            if ((rows_mask >> r) & 1u)
+                                for (int i = lane; i < left; i += 32) {
+                                    const int64_t to = (first + r) * a.M + c0 + from + i;
+                                    if (size == 2)
+                                        static_cast<uint16_t *>(a.y)[to] = *reinterpret_cast<const uint16_t *>(out + r * L::kOutPitch + i * 2);
+                                    else static_cast<uint32_t *>(a.y)[to] = *reinterpret_cast<const uint32_t *>(out + r * L::kOutPitch + i * 4);
+                                }
+                    }
+                    __syncwarp();
+                };
+                uint4 *mine_out = reinterpret_cast<uint4 *>(out + lane * L::kOutPitch);
+                if (a.out_bf16) {
 #pragma unroll
-                        for (int i = 0; i < kCols; i += 4) {
-                            if (a.vector && i + 4 <= valid) {
-                                *reinterpret_cast<float4 *>(out + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
-                            } else {
+                    for (int c = 0; c < kCols; c += 64) {
 #pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    if (i + j < valid) out[i + j] = acc[i + j];
-                            }
+                        for (int i = 0; i < 8; ++i) {
+                            const float *v = acc + c + i * 8;
+                            mine_out[i] = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
                         }
+                        flush(c, 64);
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 32) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float *v = acc + c + i * 4;
+                            mine_out[i] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                        }
+                        flush(c, 32);
                     }
                 }
             } else {
@@ -745,11 +775,11 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     }
     if (!ok && a.status) *a.status = 1u;
 
-    if constexpr (!GROUPED && !TOK) {
+    if constexpr (!GROUPED && !PAIR) {
         if (splits > 1) {
             cluster_sync();
             if (warp >= L::kFirst) {
-                const Tile tile = find_tile<N, TOK, GROUPED, PAIR>(a, prefix, n_groups, t_first, rank);
+                const Tile tile = find_tile<N, PAIR, GROUPED>(a, prefix, n_groups, t_first, rank);
                 const int row = (warp & 3) * 32 + lane;
                 const int64_t m = tile.w0 + row;
                 for (int n = rank; n < tile.rows; n += splits) {
@@ -813,23 +843,23 @@ int encode(CUtensorMap *map, const void *data, int64_t K, int64_t rows, int expe
     return BITCOS_OK;
 }
 
-template <int N, bool TOK, bool GROUPED, bool PAIR = false>
+template <int N, bool PAIR, bool GROUPED>
 int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_rows, const Fp8Args &args, int64_t blocks, cudaStream_t stream) {
-    using L = Layout<N, TOK, GROUPED, PAIR>;
-    static_assert(TOK || 2 * (L::kDynamic + 1024) <= 228 * 1024, "two blocks per multiprocessor");
+    using L = Layout<N, PAIR, GROUPED>;
+    static_assert(PAIR || 2 * (L::kDynamic + 1024) <= 228 * 1024, "two blocks per multiprocessor");
     static_assert(L::kDynamic <= 227 * 1024, "shared memory of a block");
     CUtensorMap wmap, xmap;
-    int rc = encode(&wmap, W, K, args.M, experts, TOK ? L::kBRows : kARows);
+    int rc = encode(&wmap, W, K, args.M, experts, PAIR ? L::kBRows : kARows);
     if (rc) return rc;
     rc = encode(&xmap, x, K, x_rows, 0, L::kRowsPerTile);
     if (rc) return rc;
-    auto *kernel = fp8_matmul_kernel<N, TOK, GROUPED, PAIR>;
+    auto *kernel = fp8_matmul_kernel<N, PAIR, GROUPED>;
     static bool prepared[32];                // (per device; as in prepare_kernel, and all of the cache as shared memory)
     int dev = 0;
     rc = check_cuda(cudaGetDevice(&dev));
     if (rc) return rc;
     if (dev >= 32 || !prepared[dev]) {
-        if (TOK) {
+        if (PAIR) {
             cudaFuncAttributes attributes{};
             rc = check_cuda(cudaFuncGetAttributes(&attributes, kernel));
             if (rc) return rc;
@@ -939,19 +969,12 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
     int sms = 0;
     rc = multiprocessors(&sms);
     if (rc) return rc;
-    const int64_t row_tiles = (rows + kARows - 1) / kARows, w_tiles = (M + 255) / 256;
-    const int64_t pairs = (rows + 2 * kARows - 1) / (2 * kARows);
-    if (rows > 128 && pairs * w_tiles >= sms / 4) {
-        if (pairs * w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
-        a.row_tiles = static_cast<int>(pairs);
-        a.w_tiles = static_cast<int>(w_tiles);
-        return launch_fp8<256, true, false, true>(W, x, K, 1, rows, a, 2 * std::min<int64_t>(pairs * w_tiles, sms / 2), stream);
-    }
-    if (rows > 128 && row_tiles * w_tiles >= sms / 2) {
+    const int64_t row_tiles = (rows + 255) / 256, w_tiles = (M + 255) / 256;
+    if (rows > 128 && row_tiles * w_tiles >= sms / 4) {
         if (row_tiles * w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
         a.row_tiles = static_cast<int>(row_tiles);
         a.w_tiles = static_cast<int>(w_tiles);
-        return launch_fp8<256, true, false>(W, x, K, 1, rows, a, std::min<int64_t>(row_tiles * w_tiles, sms), stream);
+        return launch_fp8<256, true, false>(W, x, K, 1, rows, a, 2 * std::min<int64_t>(row_tiles * w_tiles, sms / 2), stream);
     }
     if (rows <= 16) return launch_weights_first<16>(W, x, K, a, sms, stream);
     if (rows <= 32) return launch_weights_first<32>(W, x, K, a, sms, stream);
@@ -1008,7 +1031,7 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
     if (mean <= 16) return launch_fp8<32, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     if (mean <= 32) return launch_fp8<64, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     a.w_tiles = static_cast<int>((M + 255) / 256);
-    return launch_fp8<256, true, true>(W, x, K, n_experts, n_xrows, a, sms, stream);
+    return launch_fp8<256, true, true>(W, x, K, n_experts, n_xrows, a, sms / 2 * 2, stream);
 }
 
 }  // extern "C"
