@@ -109,7 +109,7 @@ constexpr int kMaxGroups = BITCOS_GROUP_EXPERTS_MAX;
 constexpr int kMaxSplits = 8;             // portable cluster size
 // Registers per thread, tokens first: what the block is launched with (checked before the first launch), and what the warps in
 // front and the promoters split it into.
-constexpr int kLaunchRegisters = 168, kFrontRegisters = 88, kPromoterRegisters = 208;
+constexpr int kLaunchRegisters = 168, kFrontRegisters = 72, kPromoterRegisters = 216;
 
 struct Fp8Args {
     const float *w_scale;       // [experts][w_blocks][G]
@@ -139,12 +139,19 @@ struct Tile {
 
 // PAIR (tokens first, dense): two blocks of a cluster multiply as one, 256 tokens by 256 weight rows; each loads its own 128
 // tokens and half of the weight rows.
+// The routing lists as every role of a block looks tiles up in them.
+struct GroupLists {
+    int32_t tiles[kMaxGroups + 1];         // in front of every group, and of all
+    int32_t begin[kMaxGroups + 1];
+    int32_t expert[kMaxGroups];
+};
+
 template <int N, bool PAIR, bool GROUPED>
 struct Layout {
     static constexpr int kBRows = PAIR ? N / 2 : N;     // of the B operand in this block's shared memory
     static constexpr uint32_t kBBytes = kBRows * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = PAIR ? 5 : N <= 32 ? 5 : N == 64 ? 4 : 3;
+    static constexpr int kStages = PAIR || N == 16 || (N == 32 && !GROUPED) ? 5 : N <= 64 ? 4 : 3;
     static constexpr int kParts = PAIR ? 2 : 1;          // of the accumulator's columns, one for every four promoter warps
     static constexpr int kColumns = N / kParts;         // per promoter thread
     static constexpr int kPromoters = 4 * kParts;       // warps
@@ -156,12 +163,12 @@ struct Layout {
     static constexpr uint32_t kTmemColumns = 2 * N < 32 ? 32 : 2 * N;
     // byte offsets behind the stages
     static constexpr uint32_t kBars = kStages * kStageBytes;
-    static constexpr uint32_t kTmem = kBars + (2 * kStages + 5) * 8;
+    static constexpr uint32_t kTmem = kBars + (3 * kStages + 5) * 8;
     static constexpr uint32_t kScales = (kTmem + 4 + 15) / 16 * 16;
     // PAIR: 32 rows of 128 bytes and 16 of padding per promoter warp, through which the outputs go to memory by whole lines
     static constexpr uint32_t kOutPitch = 144, kOutBytes = 32 * kOutPitch;
     static constexpr uint32_t kPrefix = kScales + (PAIR ? kPromoters * kOutBytes : kPromoters * 2 * N * 4);
-    static constexpr uint32_t kTotal = kPrefix + (GROUPED ? (kMaxGroups + 1) * 8 : 0);
+    static constexpr uint32_t kTotal = kPrefix + (GROUPED ? sizeof(GroupLists) : 0);
     static constexpr uint32_t kDynamic = kTotal + 1024;  // (the stages start on a 1024-byte boundary)
 };
 
@@ -300,8 +307,8 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank
     return a;
 }
 // (Without .release.cluster: that waits for all of the thread's memory traffic, 1000 clocks a time, and what the arrival stands for
-// is done before it goes out and is nobody else's: reads of tensor memory that tcgen05.wait::ld has seen done, or copies that
-// cp.async.wait_group has seen land in this block's shared memory, where this multiprocessor's own tensor cores read them.)
+// is done before it goes out and is nobody else's: reads of tensor memory that tcgen05.wait::ld has seen done, or copies that a
+// barrier has seen land in this block's shared memory, where this multiprocessor's own tensor cores read them.)
 __device__ __forceinline__ void cluster_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
@@ -314,7 +321,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 // that run at the same time share rows and weights in L2.  Grouped: the group by bisection in the running tile counts; inside a group
 // the tokens vary fastest (the tiles of one stretch of weights run side by side).
 template <int N, bool PAIR, bool GROUPED>
-__device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefix, int n_groups, int64_t t, int rank) {
+__device__ __forceinline__ Tile find_tile(const Fp8Args &a, const GroupLists *lists, int n_groups, int64_t t, int rank) {
     using L = Layout<N, PAIR, GROUPED>;
     Tile r;
     if constexpr (!GROUPED) {
@@ -329,20 +336,20 @@ __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const int64_t *prefi
         r.w0 = w * L::kWRowsPerTile;
         r.expert = 0;
     } else {
-        int lo = 0, hi = n_groups;                 // prefix[lo] <= t < prefix[hi]
+        int lo = 0, hi = n_groups;                 // tiles[lo] <= t < tiles[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
-            if (prefix[mid] <= t) lo = mid;
+            if (lists->tiles[mid] <= t) lo = mid;
             else hi = mid;
         }
-        const int begin = __ldg(a.group_begin + lo), end = __ldg(a.group_begin + lo + 1);
+        const int begin = lists->begin[lo], end = lists->begin[lo + 1];
         const int row_tiles = (end - begin + L::kTileRows - 1) / L::kTileRows;
-        const int in = static_cast<int>(t - prefix[lo]);
+        const int in = static_cast<int>(t) - lists->tiles[lo];
         const int w = in / row_tiles, row_tile = in - w * row_tiles;
         r.row0 = begin + static_cast<int64_t>(row_tile) * L::kTileRows + (PAIR ? rank * L::kRowsPerTile : 0);
         r.rows = max(0, min(L::kRowsPerTile, static_cast<int>(end - r.row0)));
         r.w0 = w * L::kWRowsPerTile;
-        r.expert = __ldg(a.group_expert + lo);
+        r.expert = lists->expert[lo];
     }
     return r;
 }
@@ -357,8 +364,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     uint8_t *smem = smem_raw + (1024u - (raw & 1023u)) % 1024u;
     const uint32_t base = smem_addr(smem);
     const uint32_t full = base + L::kBars, empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
-    const uint32_t drained = acc_empty + 16;
-    int64_t *prefix = reinterpret_cast<int64_t *>(smem + L::kPrefix);
+    const uint32_t drained = acc_empty + 16, gathered = drained + 8;
+    GroupLists *lists = reinterpret_cast<GroupLists *>(smem + L::kPrefix);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int splits = GROUPED || PAIR ? 1 : a.splits;
     const bool gather = GROUPED && a.pair_xrow != nullptr;
@@ -377,7 +384,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     // the first weights are on their way before the kernel in front of this one has finished: they are nobody's output
     const auto send_first = [&]() {
         if (t_first < static_cast<int64_t>(a.row_tiles) * a.w_tiles) {
-            const Tile t = find_tile<N, PAIR, GROUPED>(a, prefix, 0, t_first, rank);
+            const Tile t = find_tile<N, PAIR, GROUPED>(a, lists, 0, t_first, rank);
             for (int i = 0; i < kStages && k0 + i < k1; ++i) {
                 if (!PAIR || rank == 0) mbar_expect_tx(full + 8 * i, (PAIR ? 2 : 1) * L::kStageBytes);
                 send_weights(i, t, k0 + i, lead_full + 8 * i);
@@ -387,8 +394,9 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
 
     if (warp == 0 && elect_one()) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(full + 8 * s, gather ? (PAIR ? 5 : 3) : 1);
+            mbar_init(full + 8 * s, gather && PAIR ? 2 : 1);
             mbar_init(empty + 8 * s, 1);
+            mbar_init(gathered + 8 * s, 64);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full + 8 * b, 1);
@@ -430,6 +438,9 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 int64_t tiles = 0;
                 if (g < n_groups) {
                     const int e = __ldg(a.group_expert + g), begin = __ldg(a.group_begin + g), end = __ldg(a.group_begin + g + 1);
+                    lists->expert[g] = e;
+                    lists->begin[g] = begin;
+                    lists->begin[g + 1] = end;               // (twice the same where the next group is another lane's)
                     if (end > begin) {
                         // a malformed group is skipped whole and marked (an empty one without a mark)
                         if (e >= 0 && e < a.n_experts && begin >= 0 && end <= a.rows)
@@ -442,13 +453,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     const int64_t up = __shfl_up_sync(kFull, tiles, d);
                     if (lane >= d) tiles += up;
                 }
-                if (g < n_groups) prefix[g + 1] = sum + tiles;
+                // (groups that do not overlap have fewer tiles than 2^31, the host has seen to it; of overlapping ones the rest is left out)
+                if (g < n_groups) lists->tiles[g + 1] = static_cast<int32_t>(min(sum + tiles, static_cast<int64_t>(INT_MAX)));
                 sum += __shfl_sync(kFull, tiles, 31);
             }
-            if (lane == 0) prefix[0] = 0;
+            if (lane == 0) lists->tiles[0] = 0;
         }
         __syncthreads();
-        n_tiles = prefix[n_groups];
+        n_tiles = lists->tiles[n_groups];
     }
     constexpr uint32_t kXBytes = PAIR ? kABytes : L::kBBytes;
     bool ok = true;
@@ -462,7 +474,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         if (warp == 0) {
             // ---- producer
             for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-                const Tile tile = find_tile<N, PAIR, GROUPED>(a, prefix, n_groups, t, rank);
+                const Tile tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t, rank);
                 for (int kb = k0; ok && kb < k1; ++kb, ++it) {
                     const uint32_t s = it % kStages;
                     const uint32_t x_dst = base + s * L::kStageBytes + (PAIR ? 0 : kABytes);
@@ -494,16 +506,21 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             for (int64_t t = t_first; issues && ok && t < n_tiles; t += t_step) {
                 for (int kb = k0; kb < k1; ++kb, ++it) {
                     const uint32_t s = it % kStages, b = it & 1;
-                    // (both barriers are asked before either answer is looked at: an answer takes about 200 clocks here, and
+                    // (the barriers are asked before any answer is looked at: an answer takes about 200 clocks here, and
                     // this warp's turn has to stay below the 512 clocks of its products)
                     const uint32_t have = mbar_try(full + 8 * s, (it / kStages) & 1);
                     const uint32_t room = it < 2 || mbar_try(acc_empty + 8 * b, (it / 2 - 1) & 1);
-                    if (!__all_sync(kFull, have & room)) {
-                        if ((it >= 2 && !warp_wait(acc_empty + 8 * b, (it / 2 - 1) & 1)) || !warp_wait(full + 8 * s, (it / kStages) & 1)) {
+                    const uint32_t rows = !gather || mbar_try(gathered + 8 * s, (it / kStages) & 1);
+                    if (!__all_sync(kFull, have & room & rows)) {
+                        if ((it >= 2 && !warp_wait(acc_empty + 8 * b, (it / 2 - 1) & 1)) || !warp_wait(full + 8 * s, (it / kStages) & 1) ||
+                            (gather && !warp_wait(gathered + 8 * s, (it / kStages) & 1))) {
                             ok = false;
                             break;
                         }
                     }
+                    // (rows that other threads copied, for the tensor cores to read.  Here, and not by the copying warps: there it would
+                    // wait for all their copies under way, and no two stages would be)
+                    if (gather) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     tmem_fence_after();
                     if (elect_one()) {
                         const uint64_t da = matrix_desc(base + s * L::kStageBytes), db = matrix_desc(base + s * L::kStageBytes + kABytes);
@@ -515,6 +532,19 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     __syncwarp();
                 }
             }
+            // the second block's rows are announced to the first one's tensor cores
+            for (int64_t t = t_first; gather && !issues && ok && t < n_tiles; t += t_step) {
+                for (int kb = k0; kb < k1; ++kb, ++it) {
+                    const uint32_t s = it % kStages;
+                    if (!warp_wait(gathered + 8 * s, (it / kStages) & 1)) {
+                        ok = false;
+                        break;
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) cluster_arrive(lead_full + 8 * s);
+                }
+            }
             // nothing may be in flight when the tensor memory goes
             if (issues) {
                 if (elect_one()) mma_commit<PAIR, true>(drained);
@@ -524,29 +554,20 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         } else if (L::kFirst == 4 && warp < L::kFirst) {
             // ---- rows of routed pairs: two warps, eight lanes per row of 128 bytes, 16 bytes each, put where the 128-byte swizzle has them
             if (gather) {
-                constexpr int kOwn = L::kRowsPerTile / 8, kLag = kStages - 2;
+                constexpr int kOwn = L::kRowsPerTile / 8;
                 const int p = threadIdx.x - 64, r0 = p >> 3, chunk = p & 7;
                 const uint32_t x_off = (PAIR ? 0 : kABytes) + r0 * kGroup + ((chunk ^ (r0 & 7)) << 4);
                 const uint8_t *x = a.x + chunk * 16;
                 const int64_t K = static_cast<int64_t>(a.G) * kGroup;
-                // a stage is handed on when its copies have landed, kLag stages later
-                const auto hand_on = [&](uint32_t i) {
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (PAIR) cluster_arrive(lead_full + 8 * (i % kStages));
-                        else mbar_arrive(full + 8 * (i % kStages));
-                    }
-                };
                 for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-                    const Tile tile = find_tile<N, PAIR, GROUPED>(a, prefix, n_groups, t, rank);
-                    // what is not a row of the tile, or no row of x, reads row 0 and is dropped later
+                    const Tile tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t, rank);
+                    // (what is not a row of the tile, or no row of x, is not copied, and dropped later)
                     int src[kOwn];
 #pragma unroll
                     for (int j = 0; j < kOwn; ++j) {
                         const int i = r0 + 8 * j;
-                        const int r = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : 0;
-                        src[j] = r >= 0 && r < a.n_xrows ? r : 0;
+                        const int r = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : -1;
+                        src[j] = r < a.n_xrows ? r : -1;
                     }
                     for (int kb = k0; kb < k1; ++kb, ++it) {
                         const uint32_t s = it % kStages, dst = base + s * L::kStageBytes + x_off;
@@ -555,16 +576,13 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                             break;
                         }
 #pragma unroll
-                        for (int j = 0; j < kOwn; ++j) copy16(dst + j * 8 * kGroup, x + src[j] * K + kb * kGroup);
-                        asm volatile("cp.async.commit_group;" ::: "memory");
-                        if (it >= kLag) {
-                            asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-                            hand_on(it - kLag);
-                        }
+                        for (int j = 0; j < kOwn; ++j)
+                            if (src[j] >= 0) copy16(dst + j * 8 * kGroup, x + src[j] * K + kb * kGroup);
+                        // (arrives by itself when this thread's copies have landed)
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(gathered + 8 * s) : "memory");
                     }
                 }
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                for (uint32_t i = it > kLag ? it - kLag : 0; i < it; ++i) hand_on(i);
+                asm volatile("cp.async.wait_all;" ::: "memory");
             }
         }
     } else {
@@ -574,28 +592,49 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         const int quarter = warp & 3, part = PAIR ? (warp - L::kFirst) >> 2 : 0;
         const int row = quarter * 32 + lane;       // of A
         const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
+        // (PAIR) what a tile needs of the lists and the scales, looked up while the tile before is written out
+        Tile tile, coming;
+        int64_t xr = -1;                   // this thread's row of x (-1: none)
+        float sx0 = 0.f, sx1 = 0.f, sw0 = 0.f, sw1 = 0.f;      // the scales of the first two groups
+        const auto look_up = [&](int64_t t) {
+            coming = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t, rank);
+            xr = row < coming.rows ? coming.row0 + row : -1;
+            if (GROUPED && a.pair_xrow && xr >= 0) xr = __ldg(a.pair_xrow + xr);
+        };
+        const auto row_scales = [&]() { return a.x_scale + (xr >= 0 && (!GROUPED || xr < a.n_xrows) ? xr : 0) * a.G; };
+        const auto column_scales = [&](const Tile &t) {
+            const int block = (t.w0 + part * kCols) / kGroup;
+            return a.w_scale + (static_cast<int64_t>(t.expert) * a.w_blocks + (block < a.w_blocks ? block : 0)) * a.G;
+        };
+        const auto first_scales = [&]() {
+            const float *xs = row_scales(), *ws = column_scales(coming);
+            sx0 = __ldg(xs);
+            sw0 = __ldg(ws);
+            sx1 = a.G > 1 ? __ldg(xs + 1) : 0.f;
+            sw1 = a.G > 1 ? __ldg(ws + 1) : 0.f;
+        };
+        if (PAIR && t_first < n_tiles) {
+            look_up(t_first);
+            first_scales();
+        }
         for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-            const Tile tile = find_tile<N, PAIR, GROUPED>(a, prefix, n_groups, t, rank);
+            if (PAIR) tile = coming;
+            else tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t, rank);
             float acc[kCols];
 #pragma unroll
             for (int i = 0; i < kCols; ++i) acc[i] = 0.f;
             const float *ws = a.w_scale + (static_cast<int64_t>(tile.expert) * a.w_blocks) * a.G;
             if constexpr (PAIR) {
-                const int block = (tile.w0 + part * kCols) / kGroup;
-                const bool columns = block < a.w_blocks;
-                ws += static_cast<int64_t>(columns ? block : 0) * a.G;
                 bool mine = row < tile.rows;
-                int64_t xr = tile.row0 + row;
-                if (GROUPED && a.pair_xrow && mine) xr = __ldg(a.pair_xrow + xr);
                 if (GROUPED && mine && (xr < 0 || xr >= a.n_xrows)) {
                     mine = false;
                     if (a.status) *a.status = 2u;
                 }
-                const float *xs = a.x_scale + (mine ? xr : 0) * a.G;
+                const float *xs = row_scales();
+                ws = column_scales(tile);
                 // The columns pass 32 at a time through two buffers: while one is added, the other is on its way, across the groups
                 // too; the scales are asked for two groups ahead.
-                float scale = __ldg(xs + k0) * __ldg(ws + k0);
-                float sx = k0 + 1 < k1 ? __ldg(xs + k0 + 1) : 0.f, sw = k0 + 1 < k1 ? __ldg(ws + k0 + 1) : 0.f;
+                float scale = sx0 * sw0, sx = sx1, sw = sw1;
                 uint32_t d[2][32];
                 ok = warp_wait(acc_full + 8 * (it & 1), (it / 2) & 1);
                 if (ok) {
@@ -669,6 +708,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     __syncwarp();
                 };
                 uint4 *mine_out = reinterpret_cast<uint4 *>(out + lane * L::kOutPitch);
+                const bool more = t + t_step < n_tiles;
+                if (more) look_up(t + t_step);
                 if (a.out_bf16) {
 #pragma unroll
                     for (int c = 0; c < kCols; c += 64) {
@@ -678,6 +719,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                             mine_out[i] = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
                         }
                         flush(c, 64);
+                        if (c == 0 && more) first_scales();
                     }
                 } else {
 #pragma unroll
@@ -688,6 +730,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                             mine_out[i] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
                         }
                         flush(c, 32);
+                        if (c == 0 && more) first_scales();
                     }
                 }
             } else {
@@ -779,7 +822,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         if (splits > 1) {
             cluster_sync();
             if (warp >= L::kFirst) {
-                const Tile tile = find_tile<N, PAIR, GROUPED>(a, prefix, n_groups, t_first, rank);
+                const Tile tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t_first, rank);
                 const int row = (warp & 3) * 32 + lane;
                 const int64_t m = tile.w0 + row;
                 for (int n = rank; n < tile.rows; n += splits) {
@@ -1024,6 +1067,7 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
     // what the host knows of the groups' lengths is their mean, if all of them are there
     const int64_t mean = (n_pairs + max_groups - 1) / max_groups;
     a.w_tiles = a.w_blocks;
+    if ((n_pairs / 16 + max_groups) * a.w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
     // (no more blocks than there can be tiles)
     const int64_t most = [&](int64_t rows) { return (n_pairs / rows + std::min<int64_t>(max_groups, n_pairs)) * a.w_tiles; }(16);
     const int64_t two = std::min<int64_t>(2 * sms, most);
