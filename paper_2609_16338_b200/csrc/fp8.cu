@@ -136,9 +136,25 @@ struct Tile {
     int w0;                     // first weight row
     int expert;
 };
+// The producer hands the tiles on in a ring.  It is ahead by the stages, the two accumulators and the tile that is being written
+// out at most, less than the ring holds: nobody has to say that an entry has been read.
+constexpr int kTileRing = 16;
 
 // PAIR (tokens first, dense): two blocks of a cluster multiply as one, 256 tokens by 256 weight rows; each loads its own 128
 // tokens and half of the weight rows.
+// A place in the ring of stages and the parity of its round.  (Counted along: a remainder and a quotient at every step are 50 clocks of
+// a warp that has about 500 for one.)
+template <int STAGES>
+struct Stage {
+    uint32_t s = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == STAGES) {
+            s = 0;
+            phase ^= 1;
+        }
+    }
+};
+
 // The routing lists as every role of a block looks tiles up in them.
 struct GroupLists {
     int32_t tiles[kMaxGroups + 1];         // in front of every group, and of all
@@ -163,7 +179,9 @@ struct Layout {
     static constexpr uint32_t kTmemColumns = 2 * N < 32 ? 32 : 2 * N;
     // byte offsets behind the stages
     static constexpr uint32_t kBars = kStages * kStageBytes;
-    static constexpr uint32_t kTmem = kBars + (3 * kStages + 5) * 8;
+    static constexpr uint32_t kTiles = kBars + (3 * kStages + 5 + kTileRing) * 8;
+    static constexpr uint32_t kRows = kTiles + kTileRing * sizeof(Tile);
+    static constexpr uint32_t kTmem = kRows + (GROUPED ? kRowsPerTile * 4 : 0);
     static constexpr uint32_t kScales = (kTmem + 4 + 15) / 16 * 16;
     // PAIR: 32 rows of 128 bytes and 16 of padding per promoter warp, through which the outputs go to memory by whole lines
     static constexpr uint32_t kOutPitch = 144, kOutBytes = 32 * kOutPitch;
@@ -194,10 +212,10 @@ __device__ __forceinline__ void tma_3d_pair(uint32_t dst, const CUtensorMap *map
                  : "memory");
 }
 
-// 16 bytes from anywhere in global memory, asynchronously (the rows of routed pairs: one copy of a whole row's 128 bytes
-// by tile::gather4 costs the TMA unit about 25 clocks, 3300 a stage of 128 rows).
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// 16 bytes from anywhere in global memory, asynchronously; with there = 0 nothing is read and zeros are written.  (The rows of routed
+// pairs: tile::gather4 costs the TMA unit about 25 clocks a row of 128 bytes, 3300 a stage of 128 rows.)
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there));
 }
 
 // Shared-memory matrix descriptor: K-major rows of 128 bytes, 128-byte swizzle, eight rows (1024 bytes) apart per step.
@@ -276,8 +294,29 @@ __device__ __forceinline__ bool elect_one() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
     return one != 0;
 }
+// Asks whether a phase is complete, asleep for up to a millisecond until it is.  (Without the time a question returns at once, and ten
+// warps that keep asking leave every other access to shared memory 600 clocks in the queue.)
+__device__ __forceinline__ uint32_t ask(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity), "r"(1000000u)
+        : "memory");
+    return done;
+}
 // A bounded wait.  (No call in it: with one, ptxas keeps every role to the registers that the block is launched with.)
-__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity) { return mbar_try(bar, parity) || mbar_wait_limited(bar, parity, kWaitLimitNs); }
+__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity) {
+    uint64_t t0 = 0;
+    while (!ask(bar, parity)) {
+        const uint64_t now = global_timer_ns();
+        if (t0 == 0) t0 = now;
+        else if (now - t0 > kWaitLimitNs) return false;
+    }
+    return true;
+}
 // A bounded wait by a whole warp, which goes on or gives up as one (what follows are instructions of whole warps).
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(kFull, wait_here(bar, parity)); }
 // a += d * s, two at a time
@@ -365,6 +404,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     const uint32_t base = smem_addr(smem);
     const uint32_t full = base + L::kBars, empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
     const uint32_t drained = acc_empty + 16, gathered = drained + 8;
+    const uint32_t told = gathered + 8 * kStages;            // [kTileRing] the entry has been written
+    Tile *ring = reinterpret_cast<Tile *>(smem + L::kTiles);
     GroupLists *lists = reinterpret_cast<GroupLists *>(smem + L::kPrefix);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int splits = GROUPED || PAIR ? 1 : a.splits;
@@ -396,13 +437,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         for (int s = 0; s < kStages; ++s) {
             mbar_init(full + 8 * s, gather && PAIR ? 2 : 1);
             mbar_init(empty + 8 * s, 1);
-            mbar_init(gathered + 8 * s, 64);
+            mbar_init(gathered + 8 * s, 2);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full + 8 * b, 1);
             mbar_init(acc_empty + 8 * b, (PAIR ? 2 : 1) * L::kPromoters);
         }
         mbar_init(drained, 1);
+        for (int i = 0; i < kTileRing; ++i) mbar_init(told + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (!GROUPED && !PAIR) send_first();
     }
@@ -465,6 +507,12 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     constexpr uint32_t kXBytes = PAIR ? kABytes : L::kBBytes;
     bool ok = true;
     uint32_t it = 0;                       // groups of 128 so far, over all tiles
+    uint32_t tiles = 0;                    // tiles so far
+    const auto next_tile = [&](Tile &t) {  // the block's next tile, from the ring
+        if (!warp_wait(told + 8 * (tiles % kTileRing), (tiles / kTileRing) & 1)) return false;
+        t = ring[tiles++ % kTileRing];
+        return true;
+    };
 
     // Tokens first: a promoter holds 128 sums and 64 columns on their way; what it takes over 168 registers the four warps in
     // front give.  (In the two branches themselves: where they meet, the smaller number holds.)
@@ -473,12 +521,19 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         if (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFrontRegisters));
         if (warp == 0) {
             // ---- producer
+            Stage<kStages> at;
             for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
                 const Tile tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t, rank);
+                if (elect_one()) {
+                    ring[tiles % kTileRing] = tile;
+                    mbar_arrive(told + 8 * (tiles % kTileRing));
+                }
+                ++tiles;
+                __syncwarp();
                 for (int kb = k0; ok && kb < k1; ++kb, ++it) {
-                    const uint32_t s = it % kStages;
+                    const uint32_t s = at.s;
                     const uint32_t x_dst = base + s * L::kStageBytes + (PAIR ? 0 : kABytes);
-                    if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
+                    if (it >= kStages && !warp_wait(empty + 8 * s, at.phase ^ 1)) {
                         ok = false;
                         break;
                     }
@@ -494,6 +549,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                         }
                     }
                     __syncwarp();
+                    at.next();
                 }
             }
             // no copy may outlive the block, and (PAIR) no arrival from the other block's products: every stage has been read
@@ -502,18 +558,20 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         } else if (warp == 1) {
             // ---- tensor cores: the warp waits, one lane issues
             constexpr uint32_t idesc = instruction_desc(PAIR ? 2 * kARows : kARows, N);
+            Stage<kStages> at;
+            const uint64_t desc_a = matrix_desc(base), desc_b = matrix_desc(base + kABytes);
             const bool issues = !PAIR || rank == 0;
             for (int64_t t = t_first; issues && ok && t < n_tiles; t += t_step) {
                 for (int kb = k0; kb < k1; ++kb, ++it) {
-                    const uint32_t s = it % kStages, b = it & 1;
+                    const uint32_t s = at.s, b = it & 1;
                     // (the barriers are asked before any answer is looked at: an answer takes about 200 clocks here, and
                     // this warp's turn has to stay below the 512 clocks of its products)
-                    const uint32_t have = mbar_try(full + 8 * s, (it / kStages) & 1);
-                    const uint32_t room = it < 2 || mbar_try(acc_empty + 8 * b, (it / 2 - 1) & 1);
-                    const uint32_t rows = !gather || mbar_try(gathered + 8 * s, (it / kStages) & 1);
+                    const uint32_t have = ask(full + 8 * s, at.phase);
+                    const uint32_t room = it < 2 || ask(acc_empty + 8 * b, (it / 2 - 1) & 1);
+                    const uint32_t rows = !gather || ask(gathered + 8 * s, at.phase);
                     if (!__all_sync(kFull, have & room & rows)) {
-                        if ((it >= 2 && !warp_wait(acc_empty + 8 * b, (it / 2 - 1) & 1)) || !warp_wait(full + 8 * s, (it / kStages) & 1) ||
-                            (gather && !warp_wait(gathered + 8 * s, (it / kStages) & 1))) {
+                        if ((it >= 2 && !warp_wait(acc_empty + 8 * b, (it / 2 - 1) & 1)) || !warp_wait(full + 8 * s, at.phase) ||
+                            (gather && !warp_wait(gathered + 8 * s, at.phase))) {
                             ok = false;
                             break;
                         }
@@ -523,13 +581,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     if (gather) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     tmem_fence_after();
                     if (elect_one()) {
-                        const uint64_t da = matrix_desc(base + s * L::kStageBytes), db = matrix_desc(base + s * L::kStageBytes + kABytes);
+                        const uint64_t da = desc_a + s * (L::kStageBytes >> 4), db = desc_b + s * (L::kStageBytes >> 4);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) mma_e4m3<PAIR>(tmem + b * N, da + 2 * k, db + 2 * k, idesc, k > 0);
                         mma_commit<PAIR>(acc_full + 8 * b);
                         mma_commit<PAIR>(empty + 8 * s);
                     }
                     __syncwarp();
+                    at.next();
                 }
             }
             // the second block's rows are announced to the first one's tensor cores
@@ -554,35 +613,57 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         } else if (L::kFirst == 4 && warp < L::kFirst) {
             // ---- rows of routed pairs: two warps, eight lanes per row of 128 bytes, 16 bytes each, put where the 128-byte swizzle has them
             if (gather) {
-                constexpr int kOwn = L::kRowsPerTile / 8;
+                constexpr int kOwn = L::kRowsPerTile / 8, kLag = kStages - 2;
                 const int p = threadIdx.x - 64, r0 = p >> 3, chunk = p & 7;
                 const uint32_t x_off = (PAIR ? 0 : kABytes) + r0 * kGroup + ((chunk ^ (r0 & 7)) << 4);
                 const uint8_t *x = a.x + chunk * 16;
-                const int64_t K = static_cast<int64_t>(a.G) * kGroup;
+                const uint32_t K = static_cast<uint32_t>(a.G) * kGroup;
+                // A stage is announced when this warp's copies for it have landed: before the warp waits for room for the stage kLag later.
+                // (An arrival that the copies make themselves is one per thread, and 64 at one barrier take 900 clocks.)
+                uint32_t announced = 0;
+                Stage<kStages> ring_at, announced_at;
+                const auto announce = [&]() {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(gathered + 8 * announced_at.s);
+                    announced_at.next();
+                    ++announced;
+                };
                 for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
-                    const Tile tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t, rank);
-                    // (what is not a row of the tile, or no row of x, is not copied, and dropped later)
+                    Tile tile;
+                    if (!next_tile(tile)) {
+                        ok = false;
+                        break;
+                    }
+                    // this thread's rows: r0, r0 + 8, ... (-1: no row of the tile, or no row of x: zeros, and dropped later)
                     int src[kOwn];
 #pragma unroll
                     for (int j = 0; j < kOwn; ++j) {
                         const int i = r0 + 8 * j;
-                        const int r = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : -1;
-                        src[j] = r < a.n_xrows ? r : -1;
+                        src[j] = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : -1;
                     }
                     for (int kb = k0; kb < k1; ++kb, ++it) {
-                        const uint32_t s = it % kStages, dst = base + s * L::kStageBytes + x_off;
-                        if (it >= kStages && !warp_wait(empty + 8 * s, (it / kStages - 1) & 1)) {
+                        if (it >= kLag) {
+                            asm volatile("cp.async.wait_group %0;" ::"n"(kLag - 1) : "memory");
+                            announce();
+                        }
+                        if (it >= kStages && !warp_wait(empty + 8 * ring_at.s, ring_at.phase ^ 1)) {
                             ok = false;
                             break;
                         }
+                        const uint32_t dst = base + ring_at.s * L::kStageBytes + x_off;
+                        const uint8_t *from = x + kb * kGroup;
+                        // (no branches: a copy is a multiplication and the instruction itself)
 #pragma unroll
-                        for (int j = 0; j < kOwn; ++j)
-                            if (src[j] >= 0) copy16(dst + j * 8 * kGroup, x + src[j] * K + kb * kGroup);
-                        // (arrives by itself when this thread's copies have landed)
-                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(gathered + 8 * s) : "memory");
+                        for (int j = 0; j < kOwn; ++j) {
+                            const bool there = static_cast<uint32_t>(src[j]) < static_cast<uint32_t>(a.n_xrows);
+                            copy16(dst + j * 8 * kGroup, from + static_cast<uint64_t>(there ? static_cast<uint32_t>(src[j]) : 0u) * K, there ? 16u : 0u);
+                        }
+                        asm volatile("cp.async.commit_group;" ::: "memory");
+                        ring_at.next();
                     }
                 }
-                asm volatile("cp.async.wait_all;" ::: "memory");
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                while (announced < it) announce();
             }
         }
     } else {
@@ -592,13 +673,13 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         const int quarter = warp & 3, part = PAIR ? (warp - L::kFirst) >> 2 : 0;
         const int row = quarter * 32 + lane;       // of A
         const uint32_t tmem_row = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
-        // (PAIR) what a tile needs of the lists and the scales, looked up while the tile before is written out
+        // (PAIR) what a tile needs of the lists and the scales, asked for during the last groups of the tile before
         Tile tile, coming;
         int64_t xr = -1;                   // this thread's row of x (-1: none)
         float sx0 = 0.f, sx1 = 0.f, sw0 = 0.f, sw1 = 0.f;      // the scales of the first two groups
-        const auto look_up = [&](int64_t t) {
-            coming = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t, rank);
-            xr = row < coming.rows ? coming.row0 + row : -1;
+        const auto look_up = [&]() {
+            ok = next_tile(coming);
+            xr = ok && row < coming.rows ? coming.row0 + row : -1;
             if (GROUPED && a.pair_xrow && xr >= 0) xr = __ldg(a.pair_xrow + xr);
         };
         const auto row_scales = [&]() { return a.x_scale + (xr >= 0 && (!GROUPED || xr < a.n_xrows) ? xr : 0) * a.G; };
@@ -614,8 +695,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             sw1 = a.G > 1 ? __ldg(ws + 1) : 0.f;
         };
         if (PAIR && t_first < n_tiles) {
-            look_up(t_first);
-            first_scales();
+            look_up();
+            if (ok) first_scales();
         }
         for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
             if (PAIR) tile = coming;
@@ -635,46 +716,56 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 // The columns pass 32 at a time through two buffers: while one is added, the other is on its way, across the groups
                 // too; the scales are asked for two groups ahead.
                 float scale = sx0 * sw0, sx = sx1, sw = sw1;
+                const bool more = t + t_step < n_tiles;
                 uint32_t d[2][32];
                 ok = warp_wait(acc_full + 8 * (it & 1), (it / 2) & 1);
                 if (ok) {
                     tmem_fence_after();
                     tmem_load32(tmem_row + (it & 1) * N, d[0]);
                 }
-                for (int kb = k0; ok && kb < k1; ++kb) {
-                    const uint32_t b = it & 1;
-                    const float s = scale;
-                    scale = sx * sw;
-                    if (kb + 2 < k1) {
-                        sx = __ldg(xs + kb + 2);
-                        sw = __ldg(ws + kb + 2);
-                    }
-                    ++it;
-                    uint32_t next = 1;
+                // (in three runs, so that looking ahead to the next tile costs the loop itself nothing)
+                int kb = k0;
+#pragma unroll 1
+                for (int run = 0; run < 3; ++run) {
+                    const int stop = run == 0 ? max(k0, k1 - 3) : run == 1 ? max(k0, k1 - 1) : k1;
+#pragma unroll 1
+                    for (; ok && kb < stop; ++kb) {
+                        const uint32_t b = it & 1;
+                        const float s = scale;
+                        scale = sx * sw;
+                        if (kb + 2 < k1) {
+                            sx = __ldg(xs + kb + 2);
+                            sw = __ldg(ws + kb + 2);
+                        }
+                        ++it;
+                        uint32_t next = 1;
 #pragma unroll
-                    for (int c = 0; c < kCols / 32; ++c) {
-                        tmem_wait32(d[c & 1]);
-                        if (c + 1 < kCols / 32) {
-                            tmem_load32(tmem_row + b * N + (c + 1) * 32, d[(c + 1) & 1]);
-                        } else {
-                            tmem_fence_before();
-                            __syncwarp();
-                            if (lane == 0) {
-                                if constexpr (PAIR) cluster_arrive(lead_acc_empty + 8 * b);
-                                else mbar_arrive(acc_empty + 8 * b);
+                        for (int c = 0; c < kCols / 32; ++c) {
+                            tmem_wait32(d[c & 1]);
+                            if (c + 1 < kCols / 32) {
+                                tmem_load32(tmem_row + b * N + (c + 1) * 32, d[(c + 1) & 1]);
+                            } else {
+                                tmem_fence_before();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    if constexpr (PAIR) cluster_arrive(lead_acc_empty + 8 * b);
+                                    else mbar_arrive(acc_empty + 8 * b);
+                                }
+                                if (kb + 1 < k1) next = ask(acc_full + 8 * (it & 1), (it / 2) & 1);
                             }
-                            if (kb + 1 < k1) next = mbar_try(acc_full + 8 * (it & 1), (it / 2) & 1);
-                        }
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) fma_pair(acc[c * 32 + i], acc[c * 32 + i + 1], d[c & 1][i], d[c & 1][i + 1], s, s);
-                    }
-                    if (kb + 1 < k1) {
-                        ok = __all_sync(kFull, next) || warp_wait(acc_full + 8 * (it & 1), (it / 2) & 1);
-                        if (ok) {
-                            tmem_fence_after();
-                            tmem_load32(tmem_row + (it & 1) * N, d[0]);
+                            for (int i = 0; i < 32; i += 2) fma_pair(acc[c * 32 + i], acc[c * 32 + i + 1], d[c & 1][i], d[c & 1][i + 1], s, s);
+                        }
+                        if (kb + 1 < k1) {
+                            ok = __all_sync(kFull, next) || warp_wait(acc_full + 8 * (it & 1), (it / 2) & 1);
+                            if (ok) {
+                                tmem_fence_after();
+                                tmem_load32(tmem_row + (it & 1) * N, d[0]);
+                            }
                         }
                     }
+                    if (more && ok && run == 0) look_up();
+                    if (more && ok && run == 1) first_scales();
                 }
                 if (!ok) break;
                 const int64_t c0 = tile.w0 + part * kCols;
@@ -708,8 +799,6 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     __syncwarp();
                 };
                 uint4 *mine_out = reinterpret_cast<uint4 *>(out + lane * L::kOutPitch);
-                const bool more = t + t_step < n_tiles;
-                if (more) look_up(t + t_step);
                 if (a.out_bf16) {
 #pragma unroll
                     for (int c = 0; c < kCols; c += 64) {
@@ -719,7 +808,6 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                             mine_out[i] = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
                         }
                         flush(c, 64);
-                        if (c == 0 && more) first_scales();
                     }
                 } else {
 #pragma unroll
@@ -730,7 +818,6 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                             mine_out[i] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
                         }
                         flush(c, 32);
-                        if (c == 0 && more) first_scales();
                     }
                 }
             } else {
@@ -889,6 +976,7 @@ int encode(CUtensorMap *map, const void *data, int64_t K, int64_t rows, int expe
 template <int N, bool PAIR, bool GROUPED>
 int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_rows, const Fp8Args &args, int64_t blocks, cudaStream_t stream) {
     using L = Layout<N, PAIR, GROUPED>;
+    static_assert(L::kStages + 3 < kTileRing, "the producer's lead");
     static_assert(PAIR || 2 * (L::kDynamic + 1024) <= 228 * 1024, "two blocks per multiprocessor");
     static_assert(L::kDynamic <= 227 * 1024, "shared memory of a block");
     CUtensorMap wmap, xmap;
