@@ -181,7 +181,7 @@ struct Layout {
     static constexpr uint32_t kBars = kStages * kStageBytes;
     static constexpr uint32_t kTiles = kBars + (3 * kStages + 5 + kTileRing) * 8;
     static constexpr uint32_t kRows = kTiles + kTileRing * sizeof(Tile);
-    static constexpr uint32_t kTmem = kRows + (GROUPED ? kRowsPerTile * 4 : 0);
+    static constexpr uint32_t kTmem = kRows + (GROUPED ? 2 * kRowsPerTile * 4 : 0);
     static constexpr uint32_t kScales = (kTmem + 4 + 15) / 16 * 16;
     // PAIR: 32 rows of 128 bytes and 16 of padding per promoter warp, through which the outputs go to memory by whole lines
     static constexpr uint32_t kOutPitch = 144, kOutBytes = 32 * kOutPitch;
@@ -437,7 +437,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         for (int s = 0; s < kStages; ++s) {
             mbar_init(full + 8 * s, gather && PAIR ? 2 : 1);
             mbar_init(empty + 8 * s, 1);
-            mbar_init(gathered + 8 * s, 2);
+            mbar_init(gathered + 8 * s, 32);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full + 8 * b, 1);
@@ -611,59 +611,55 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 ok &= warp_wait(drained, 0);
             }
         } else if (L::kFirst == 4 && warp < L::kFirst) {
-            // ---- rows of routed pairs: two warps, eight lanes per row of 128 bytes, 16 bytes each, put where the 128-byte swizzle has them
+            // ---- rows of routed pairs: two warps take the stages in turn; eight lanes per row of 128 bytes, 16 bytes each, put where the
+            // 128-byte swizzle has them.  Bound by the copies: 512 bytes take an instruction of these about 18 clocks.
             if (gather) {
-                constexpr int kOwn = L::kRowsPerTile / 8, kLag = kStages - 2;
-                const int p = threadIdx.x - 64, r0 = p >> 3, chunk = p & 7;
-                const uint32_t x_off = (PAIR ? 0 : kABytes) + r0 * kGroup + ((chunk ^ (r0 & 7)) << 4);
+                constexpr int kOwn = L::kRowsPerTile / 4, kBatch = kOwn < 16 ? kOwn : 16;
+                const uint32_t turn = warp - 2;
+                const int r0 = lane >> 3, chunk = lane & 7;
+                const uint32_t x_off = (PAIR ? 0 : kABytes) + r0 * kGroup;
+                const uint32_t swizzled[2] = {static_cast<uint32_t>((chunk ^ r0) << 4), static_cast<uint32_t>((chunk ^ (r0 + 4)) << 4)};
                 const uint8_t *x = a.x + chunk * 16;
                 const uint32_t K = static_cast<uint32_t>(a.G) * kGroup;
-                // A stage is announced when this warp's copies for it have landed: before the warp waits for room for the stage kLag later.
-                // (An arrival that the copies make themselves is one per thread, and 64 at one barrier take 900 clocks.)
-                uint32_t announced = 0;
-                Stage<kStages> ring_at, announced_at;
-                const auto announce = [&]() {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(gathered + 8 * announced_at.s);
-                    announced_at.next();
-                    ++announced;
-                };
+                Stage<kStages> at;
+                // the tile's rows (-1: no row of the tile, or no row of x: zeros, and dropped later), a list per warp
+                int32_t *rows = reinterpret_cast<int32_t *>(smem + L::kRows) + turn * L::kRowsPerTile;
                 for (int64_t t = t_first; ok && t < n_tiles; t += t_step) {
                     Tile tile;
                     if (!next_tile(tile)) {
                         ok = false;
                         break;
                     }
-                    // this thread's rows: r0, r0 + 8, ... (-1: no row of the tile, or no row of x: zeros, and dropped later)
-                    int src[kOwn];
-#pragma unroll
-                    for (int j = 0; j < kOwn; ++j) {
-                        const int i = r0 + 8 * j;
-                        src[j] = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : -1;
+                    __syncwarp();                        // (the list is read no more)
+                    for (int i = lane; i < L::kRowsPerTile; i += 32) {
+                        const int r = i < tile.rows ? __ldg(a.pair_xrow + tile.row0 + i) : -1;
+                        rows[i] = r < a.n_xrows ? r : -1;
                     }
-                    for (int kb = k0; kb < k1; ++kb, ++it) {
-                        if (it >= kLag) {
-                            asm volatile("cp.async.wait_group %0;" ::"n"(kLag - 1) : "memory");
-                            announce();
-                        }
-                        if (it >= kStages && !warp_wait(empty + 8 * ring_at.s, ring_at.phase ^ 1)) {
+                    __syncwarp();
+                    for (int kb = k0; kb < k1; ++kb, ++it, at.next()) {
+                        if ((it & 1) != turn) continue;
+                        if (it >= kStages && !warp_wait(empty + 8 * at.s, at.phase ^ 1)) {
                             ok = false;
                             break;
                         }
-                        const uint32_t dst = base + ring_at.s * L::kStageBytes + x_off;
+                        const uint32_t dst = base + at.s * L::kStageBytes + x_off;
                         const uint8_t *from = x + kb * kGroup;
                         // (no branches: a copy is a multiplication and the instruction itself)
 #pragma unroll
-                        for (int j = 0; j < kOwn; ++j) {
-                            const bool there = static_cast<uint32_t>(src[j]) < static_cast<uint32_t>(a.n_xrows);
-                            copy16(dst + j * 8 * kGroup, from + static_cast<uint64_t>(there ? static_cast<uint32_t>(src[j]) : 0u) * K, there ? 16u : 0u);
+                        for (int j0 = 0; j0 < kOwn; j0 += kBatch) {
+                            int src[kBatch];
+#pragma unroll
+                            for (int j = 0; j < kBatch; ++j) src[j] = rows[r0 + 4 * (j0 + j)];
+#pragma unroll
+                            for (int j = 0; j < kBatch; ++j)
+                                copy16(dst + (j0 + j) * 4 * kGroup + swizzled[j & 1],
+                                       from + static_cast<uint64_t>(static_cast<uint32_t>(max(src[j], 0))) * K, src[j] >= 0 ? 16u : 0u);
                         }
-                        asm volatile("cp.async.commit_group;" ::: "memory");
-                        ring_at.next();
+                        // (arrives by itself when this thread's copies have landed)
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(gathered + 8 * at.s) : "memory");
                     }
                 }
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                while (announced < it) announce();
+                asm volatile("cp.async.wait_all;" ::: "memory");
             }
         }
     } else {
