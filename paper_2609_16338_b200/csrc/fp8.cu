@@ -167,7 +167,7 @@ struct Layout {
     static constexpr int kBRows = PAIR ? N / 2 : N;     // of the B operand in this block's shared memory
     static constexpr uint32_t kBBytes = kBRows * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = PAIR || N == 16 || (N == 32 && !GROUPED) ? 5 : N <= 64 ? 4 : 3;
+    static constexpr int kStages = PAIR || N == 16 || (N == 32 && !GROUPED) ? 5 : 4;
     static constexpr int kParts = PAIR ? 2 : 1;          // of the accumulator's columns, one for every four promoter warps
     static constexpr int kColumns = N / kParts;         // per promoter thread
     static constexpr int kPromoters = 4 * kParts;       // warps
@@ -329,9 +329,12 @@ __device__ __forceinline__ void fma_pair(float &a0, float &a1, uint32_t d0, uint
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ __forceinline__ float cluster_load(uint32_t addr, uint32_t rank) {
-    float v;
-    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(addr), "r"(rank) : "memory");
+__device__ __forceinline__ float4 cluster_load(uint32_t addr, uint32_t rank) {
+    float4 v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr), "r"(rank)
+                 : "memory");
     return v;
 }
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -824,8 +827,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 float *scales = reinterpret_cast<float *>(smem + L::kScales) + (warp - L::kFirst) * 2 * N;
                 const float *xs[kOwn];
                 uint32_t bad[kOwn];                // columns whose row of x does not exist: not written
-                float sx[kOwn];
-                float sw = __ldg(ws + k0);
+                float sx[kOwn], sx_next[kOwn];     // the scales of this group and the next, the one after is asked for
+                float sw = __ldg(ws + k0), sw_next = k0 + 1 < k1 ? __ldg(ws + k0 + 1) : 0.f;
 #pragma unroll
                 for (int j = 0; j < kOwn; ++j) {
                     const int n = lane + 32 * j;
@@ -840,40 +843,53 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     }
                     xs[j] = there ? a.x_scale + xr * a.G : nullptr;
                     sx[j] = there ? __ldg(xs[j] + k0) : 0.f;
+                    sx_next[j] = there && k0 + 1 < k1 ? __ldg(xs[j] + k0 + 1) : 0.f;
                 }
+#pragma unroll 1
                 for (int kb = k0; kb < k1; ++kb, ++it) {
                     const uint32_t b = it & 1;
                     float *scale = scales + b * N;
 #pragma unroll
                     for (int j = 0; j < kOwn; ++j) {
                         if (N % 32 == 0 || lane < N) scale[lane + 32 * j] = sx[j] * sw;
-                        if (kb + 1 < k1 && xs[j]) sx[j] = __ldg(xs[j] + kb + 1);
+                        sx[j] = sx_next[j];
+                        if (kb + 2 < k1 && xs[j]) sx_next[j] = __ldg(xs[j] + kb + 2);
                     }
-                    if (kb + 1 < k1) sw = __ldg(ws + kb + 1);
+                    sw = sw_next;
+                    if (kb + 2 < k1) sw_next = __ldg(ws + kb + 2);
                     __syncwarp();
                     if (!warp_wait(acc_full + 8 * b, (it / 2) & 1)) {
                         ok = false;
                         break;
                     }
                     tmem_fence_after();
-                    uint32_t d[2][16];
-                    tmem_load16(tmem_row + b * N, d[0]);
-                    tmem_wait16(d[0]);
+                    // as many columns at once as the registers hold (all of them but in the grouped kernel of 64 tokens), so that the
+                    // accumulator goes back before they are added
+                    constexpr int kWide = kCols < 32 ? 16 : 32, kLoads = GROUPED || kCols <= kWide ? 1 : kCols / kWide;
 #pragma unroll
-                    for (int c = 0; c < kCols / 16; ++c) {
-                        if (c + 1 < kCols / 16) tmem_load16(tmem_row + b * N + (c + 1) * 16, d[(c + 1) & 1]);
-                        if (kCols == 16 || c + 1 == kCols / 16) {
+                    for (int from = 0; from < kCols; from += kWide * kLoads) {
+                        uint32_t d[kLoads][kWide];
+#pragma unroll
+                        for (int c = 0; c < kLoads; ++c) {
+                            if constexpr (kWide == 16) tmem_load16(tmem_row + b * N + from + c * kWide, d[c]);
+                            else tmem_load32(tmem_row + b * N + from + c * kWide, d[c]);
+                        }
+#pragma unroll
+                        for (int c = 0; c < kLoads; ++c) {
+                            if constexpr (kWide == 16) tmem_wait16(d[c]);
+                            else tmem_wait32(d[c]);
+                        }
+                        if (from + kWide * kLoads == kCols) {
                             tmem_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive(acc_empty + 8 * b);
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            const float4 sc = *reinterpret_cast<const float4 *>(scale + c * 16 + i);
-                            fma_pair(acc[c * 16 + i], acc[c * 16 + i + 1], d[c & 1][i], d[c & 1][i + 1], sc.x, sc.y);
-                            fma_pair(acc[c * 16 + i + 2], acc[c * 16 + i + 3], d[c & 1][i + 2], d[c & 1][i + 3], sc.z, sc.w);
+                        for (int i = 0; i < kWide * kLoads; i += 4) {
+                            const float4 sc = *reinterpret_cast<const float4 *>(scale + from + i);
+                            fma_pair(acc[from + i], acc[from + i + 1], d[i / kWide][i % kWide], d[i / kWide][i % kWide + 1], sc.x, sc.y);
+                            fma_pair(acc[from + i + 2], acc[from + i + 3], d[i / kWide][i % kWide + 2], d[i / kWide][i % kWide + 3], sc.z, sc.w);
                         }
-                        if (c + 1 < kCols / 16) tmem_wait16(d[(c + 1) & 1]);
                     }
                 }
                 if (!ok) break;
@@ -905,16 +921,30 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         if (splits > 1) {
             cluster_sync();
             if (warp >= L::kFirst) {
+                // a warp adds a token's 128 rows, four a lane; the blocks of the cluster share out the tokens
                 const Tile tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t_first, rank);
-                const int row = (warp & 3) * 32 + lane;
-                const int64_t m = tile.w0 + row;
-                for (int n = rank; n < tile.rows; n += splits) {
-                    float sum = 0.f;
-                    for (int r = 0; r < splits; ++r) sum += cluster_load(base + static_cast<uint32_t>(n * kARows + row) * 4u, r);
+                const int64_t m = tile.w0 + lane * 4;
+                for (int n = rank + splits * (warp - L::kFirst); n < tile.rows; n += splits * L::kPromoters) {
+                    float4 part[kMaxSplits];
+#pragma unroll
+                    for (int r = 0; r < kMaxSplits; ++r)
+                        if (r < splits) part[r] = cluster_load(base + static_cast<uint32_t>(n * kARows + lane * 4) * 4u, r);
+                    float4 sum = part[0];
+#pragma unroll
+                    for (int r = 1; r < kMaxSplits; ++r)
+                        if (r < splits) sum = make_float4(sum.x + part[r].x, sum.y + part[r].y, sum.z + part[r].z, sum.w + part[r].w);
                     const int64_t at = (tile.row0 + n) * a.M + m;
-                    if (m < a.M) {
-                        if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.y)[at] = __float2bfloat16_rn(sum);
-                        else static_cast<float *>(a.y)[at] = sum;
+                    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+                    if (a.vector && m < a.M) {               // (M is a multiple of four, or of eight)
+                        if (a.out_bf16) *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.y) + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+                        else *reinterpret_cast<float4 *>(static_cast<float *>(a.y) + at) = sum;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (m + i < a.M) {
+                                if (a.out_bf16) static_cast<__nv_bfloat16 *>(a.y)[at + i] = __float2bfloat16_rn(v[i]);
+                                else static_cast<float *>(a.y)[at + i] = v[i];
+                            }
                     }
                 }
             }
@@ -969,6 +999,30 @@ int encode(CUtensorMap *map, const void *data, int64_t K, int64_t rows, int expe
     return BITCOS_OK;
 }
 
+// Once per kernel and device, as in prepare_kernel, and all of the cache as shared memory.
+template <int N, bool PAIR, bool GROUPED>
+int prepare_fp8(int dev) {
+    using L = Layout<N, PAIR, GROUPED>;
+    auto *kernel = fp8_matmul_kernel<N, PAIR, GROUPED>;
+    static bool prepared[32];
+    if (dev < 32 && prepared[dev]) return BITCOS_OK;
+    int rc = BITCOS_OK;
+    if (PAIR) {
+        cudaFuncAttributes attributes{};
+        rc = check_cuda(cudaFuncGetAttributes(&attributes, kernel));
+        if (rc) return rc;
+        if (attributes.numRegs != kLaunchRegisters) {          // (the split would wait for registers that are not there)
+            g_last_cuda_error = cudaErrorInvalidDeviceFunction;
+            return BITCOS_ERR_CUDA;
+        }
+    }
+    rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kDynamic)));
+    if (rc == BITCOS_OK)
+        rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+    if (rc == BITCOS_OK && dev < 32) prepared[dev] = true;
+    return rc;
+}
+
 template <int N, bool PAIR, bool GROUPED>
 int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_rows, const Fp8Args &args, int64_t blocks, cudaStream_t stream) {
     using L = Layout<N, PAIR, GROUPED>;
@@ -981,26 +1035,10 @@ int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_r
     rc = encode(&xmap, x, K, x_rows, 0, L::kRowsPerTile);
     if (rc) return rc;
     auto *kernel = fp8_matmul_kernel<N, PAIR, GROUPED>;
-    static bool prepared[32];                // (per device; as in prepare_kernel, and all of the cache as shared memory)
     int dev = 0;
     rc = check_cuda(cudaGetDevice(&dev));
+    if (rc == BITCOS_OK) rc = prepare_fp8<N, PAIR, GROUPED>(dev);
     if (rc) return rc;
-    if (dev >= 32 || !prepared[dev]) {
-        if (PAIR) {
-            cudaFuncAttributes attributes{};
-            rc = check_cuda(cudaFuncGetAttributes(&attributes, kernel));
-            if (rc) return rc;
-            if (attributes.numRegs != kLaunchRegisters) {          // (the split would wait for registers that are not there)
-                g_last_cuda_error = cudaErrorInvalidDeviceFunction;
-                return BITCOS_ERR_CUDA;
-            }
-        }
-        rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(L::kDynamic)));
-        if (rc == BITCOS_OK)
-            rc = check_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
-        if (rc) return rc;
-        if (dev < 32) prepared[dev] = true;
-    }
     static const char *env = std::getenv("BITCOS_PDL");
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
@@ -1034,15 +1072,60 @@ int multiprocessors(int *sms) {
     return rc;
 }
 
-// Dense, weights first: as many shares of K as fill two blocks per multiprocessor, two groups of 128 each at least.
+// Dense, weights first: into how many shares K is cut, and the nanoseconds expected of it.  A block takes 270, 310 or 490 ns for a group
+// of 128 at 16, 32 and 64 tokens (640 rows, K = 6400 and 25600), or, with all multiprocessors at it, what memory needs for its
+// 16 KB; start, first copies and the cluster's sum cost 2 us more per round.  The clusters that the device holds at once are asked for
+// once per kernel and device (of seven blocks there are 30: 40 row blocks of 5120 x 25600 took two rounds and 36 us).
+constexpr int64_t kGroupNs16 = 270, kGroupNs32 = 310, kGroupNs64 = 490, kRoundNs = 2000, kPairGroupNs = 410, kPairNs = 3500;
+template <int N>
+int plan_weights_first(const Fp8Args &a, int sms, int *splits_out, int64_t *ns_out) {
+    const int64_t tiles = (a.rows + N - 1) / N * a.w_blocks;
+    if (tiles > INT_MAX / kMaxSplits) return BITCOS_ERR_SHAPE;
+    static int held[32][kMaxSplits + 1];
+    int dev = 0;
+    int rc = check_cuda(cudaGetDevice(&dev));
+    if (rc) return rc;
+    rc = prepare_fp8<N, false, false>(dev);
+    if (rc) return rc;
+    constexpr int64_t group_ns = N == 16 ? kGroupNs16 : N == 32 ? kGroupNs32 : kGroupNs64;
+    *ns_out = INT64_MAX;
+    for (int splits = 1; splits <= kMaxSplits && (splits == 1 || a.G / splits >= 2); ++splits) {
+        int clusters = dev < 32 ? held[dev][splits] : 0;
+        if (clusters == 0) {
+            cudaLaunchConfig_t cfg{};
+            cudaLaunchAttribute attr{};
+            cfg.gridDim = dim3(static_cast<unsigned>(splits));
+            cfg.blockDim = dim3(Layout<N, false, false>::kThreads);
+            cfg.dynamicSmemBytes = Layout<N, false, false>::kDynamic;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = static_cast<unsigned>(splits);
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            rc = check_cuda(cudaOccupancyMaxActiveClusters(&clusters, fp8_matmul_kernel<N, false, false>, &cfg));
+            if (rc) return rc;
+            clusters = 2 * std::max(clusters, 1);      // (it counts one block per multiprocessor, of any size; two are there)
+            if (dev < 32) held[dev][splits] = clusters;
+        }
+        const int64_t rounds = (tiles + clusters - 1) / clusters, active = std::min<int64_t>(tiles, clusters) * splits;
+        const int64_t memory_ns = active * 730 / (2 * sms);                   // 16 KB each at 6.5 TB/s
+        const int64_t ns = rounds * (kRoundNs + (a.G + splits - 1) / splits * std::max(group_ns, memory_ns));
+        if (ns < *ns_out) {
+            *ns_out = ns;
+            *splits_out = splits;
+        }
+    }
+    return BITCOS_OK;
+}
 template <int N>
 int launch_weights_first(const void *W, const void *x, int64_t K, Fp8Args &a, int sms, cudaStream_t stream) {
-    const int64_t row_tiles = (a.rows + N - 1) / N, tiles = row_tiles * a.w_blocks;
-    if (tiles > INT_MAX / kMaxSplits) return BITCOS_ERR_SHAPE;
+    int64_t ns = 0;
+    const int rc = plan_weights_first<N>(a, sms, &a.splits, &ns);
+    if (rc) return rc;
+    const int64_t row_tiles = (a.rows + N - 1) / N;
     a.row_tiles = static_cast<int>(row_tiles);
     a.w_tiles = a.w_blocks;
-    a.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, a.G / 2, 2 * sms / tiles})));
-    return launch_fp8<N, false, false>(W, x, K, 1, a.rows, a, tiles * a.splits, stream);
+    return launch_fp8<N, false, false>(W, x, K, 1, a.rows, a, row_tiles * a.w_blocks * a.splits, stream);
 }
 
 int status_word(void *workspace, size_t workspace_bytes, unsigned int **status) {
@@ -1097,7 +1180,16 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
     rc = multiprocessors(&sms);
     if (rc) return rc;
     const int64_t row_tiles = (rows + 255) / 256, w_tiles = (M + 255) / 256;
-    if (rows > 128 && row_tiles * w_tiles >= sms / 4) {
+    bool pairs = rows > 512;
+    if (rows > 64 && !pairs) {
+        // few rows: whichever ends sooner
+        int splits = 0;
+        int64_t ns = 0;
+        rc = plan_weights_first<64>(a, sms, &splits, &ns);
+        if (rc) return rc;
+        pairs = kPairNs + (row_tiles * w_tiles + sms / 2 - 1) / (sms / 2) * a.G * kPairGroupNs <= ns;
+    }
+    if (pairs) {
         if (row_tiles * w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
         a.row_tiles = static_cast<int>(row_tiles);
         a.w_tiles = static_cast<int>(w_tiles);
@@ -1105,8 +1197,7 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
     }
     if (rows <= 16) return launch_weights_first<16>(W, x, K, a, sms, stream);
     if (rows <= 32) return launch_weights_first<32>(W, x, K, a, sms, stream);
-    if (rows <= 64) return launch_weights_first<64>(W, x, K, a, sms, stream);
-    return launch_weights_first<128>(W, x, K, a, sms, stream);
+    return launch_weights_first<64>(W, x, K, a, sms, stream);
 }
 
 int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_experts, int64_t M, int64_t K, const int32_t *group_expert,
