@@ -168,7 +168,8 @@ struct Layout {
     static constexpr uint32_t kBBytes = kBRows * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = PAIR || N == 16 || (N == 32 && !GROUPED) ? 5 : 4;
-    static constexpr int kParts = PAIR ? 2 : 1;          // of the accumulator's columns, one for every four promoter warps
+    static constexpr int kParts = PAIR ? 2 : 1;          // of an accumulator's columns, one for every four promoter warps
+    static constexpr int kAcc = PAIR ? 2 : 4;            // accumulators in turn
     static constexpr int kColumns = N / kParts;         // per promoter thread
     static constexpr int kPromoters = 4 * kParts;       // warps
     static constexpr int kFirst = GROUPED || PAIR ? 4 : 2;      // the first of them (in front: TMA, tensor cores, two for gathered rows)
@@ -176,10 +177,10 @@ struct Layout {
     static constexpr int kRowsPerTile = PAIR ? kARows : N;              // tokens of a tile in this block
     static constexpr int kTileRows = PAIR ? 2 * kRowsPerTile : kRowsPerTile;
     static constexpr int kWRowsPerTile = PAIR ? N : kARows;
-    static constexpr uint32_t kTmemColumns = 2 * N < 32 ? 32 : 2 * N;
+    static constexpr uint32_t kTmemColumns = kAcc * N;
     // byte offsets behind the stages
     static constexpr uint32_t kBars = kStages * kStageBytes;
-    static constexpr uint32_t kTiles = kBars + (3 * kStages + 5 + kTileRing) * 8;
+    static constexpr uint32_t kTiles = kBars + (3 * kStages + 2 * kAcc + 1 + kTileRing) * 8;
     static constexpr uint32_t kRows = kTiles + kTileRing * sizeof(Tile);
     static constexpr uint32_t kTmem = kRows + (GROUPED ? 2 * kRowsPerTile * 4 : 0);
     static constexpr uint32_t kScales = (kTmem + 4 + 15) / 16 * 16;
@@ -307,6 +308,18 @@ __device__ __forceinline__ uint32_t ask(uint32_t bar, uint32_t parity) {
         : "memory");
     return done;
 }
+// Asks without waiting.
+__device__ __forceinline__ uint32_t test(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
 // A bounded wait.  (No call in it: with one, ptxas keeps every role to the registers that the block is launched with.)
 __device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity) {
     uint64_t t0 = 0;
@@ -405,8 +418,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     const uint32_t raw = smem_addr(smem_raw);
     uint8_t *smem = smem_raw + (1024u - (raw & 1023u)) % 1024u;
     const uint32_t base = smem_addr(smem);
-    const uint32_t full = base + L::kBars, empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 16;
-    const uint32_t drained = acc_empty + 16, gathered = drained + 8;
+    const uint32_t full = base + L::kBars, empty = full + 8 * kStages, acc_full = empty + 8 * kStages, acc_empty = acc_full + 8 * L::kAcc;
+    const uint32_t drained = acc_empty + 8 * L::kAcc, gathered = drained + 8;
     const uint32_t told = gathered + 8 * kStages;            // [kTileRing] the entry has been written
     Tile *ring = reinterpret_cast<Tile *>(smem + L::kTiles);
     GroupLists *lists = reinterpret_cast<GroupLists *>(smem + L::kPrefix);
@@ -442,7 +455,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             mbar_init(empty + 8 * s, 1);
             mbar_init(gathered + 8 * s, 32);
         }
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < L::kAcc; ++b) {
             mbar_init(acc_full + 8 * b, 1);
             mbar_init(acc_empty + 8 * b, (PAIR ? 2 : 1) * L::kPromoters);
         }
@@ -475,6 +488,13 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     int n_groups = 0;
     int64_t n_tiles = static_cast<int64_t>(a.row_tiles) * a.w_tiles;
     if constexpr (GROUPED) {
+        // (the first 32 groups are asked for together with their number: one trip to memory less)
+        int e0 = 0, begin0 = 0, end0 = 0;
+        if (warp == 0 && lane < a.max_groups) {
+            e0 = __ldg(a.group_expert + lane);
+            begin0 = __ldg(a.group_begin + lane);
+            end0 = __ldg(a.group_begin + lane + 1);
+        }
         n_groups = min(max(__ldg(a.n_groups), 0), a.max_groups);
         if (warp == 0) {
             int64_t sum = 0;
@@ -482,7 +502,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 const int g = g0 + lane;
                 int64_t tiles = 0;
                 if (g < n_groups) {
-                    const int e = __ldg(a.group_expert + g), begin = __ldg(a.group_begin + g), end = __ldg(a.group_begin + g + 1);
+                    const int e = g0 ? __ldg(a.group_expert + g) : e0, begin = g0 ? __ldg(a.group_begin + g) : begin0;
+                    const int end = g0 ? __ldg(a.group_begin + g + 1) : end0;
                     lists->expert[g] = e;
                     lists->begin[g] = begin;
                     lists->begin[g + 1] = end;               // (twice the same where the next group is another lane's)
@@ -566,14 +587,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             const bool issues = !PAIR || rank == 0;
             for (int64_t t = t_first; issues && ok && t < n_tiles; t += t_step) {
                 for (int kb = k0; kb < k1; ++kb, ++it) {
-                    const uint32_t s = at.s, b = it & 1;
+                    const uint32_t s = at.s, b = it % L::kAcc, again = (it / L::kAcc & 1) ^ 1;
                     // (the barriers are asked before any answer is looked at: an answer takes about 200 clocks here, and
                     // this warp's turn has to stay below the 512 clocks of its products)
                     const uint32_t have = ask(full + 8 * s, at.phase);
-                    const uint32_t room = it < 2 || ask(acc_empty + 8 * b, (it / 2 - 1) & 1);
                     const uint32_t rows = !gather || ask(gathered + 8 * s, at.phase);
+                    const uint32_t room = it < L::kAcc || ask(acc_empty + 8 * b, again);
                     if (!__all_sync(kFull, have & room & rows)) {
-                        if ((it >= 2 && !warp_wait(acc_empty + 8 * b, (it / 2 - 1) & 1)) || !warp_wait(full + 8 * s, at.phase) ||
+                        if ((it >= L::kAcc && !warp_wait(acc_empty + 8 * b, again)) || !warp_wait(full + 8 * s, at.phase) ||
                             (gather && !warp_wait(gathered + 8 * s, at.phase))) {
                             ok = false;
                             break;
@@ -717,10 +738,10 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 float scale = sx0 * sw0, sx = sx1, sw = sw1;
                 const bool more = t + t_step < n_tiles;
                 uint32_t d[2][32];
-                ok = warp_wait(acc_full + 8 * (it & 1), (it / 2) & 1);
+                ok = warp_wait(acc_full + 8 * (it % L::kAcc), (it / L::kAcc) & 1);
                 if (ok) {
                     tmem_fence_after();
-                    tmem_load32(tmem_row + (it & 1) * N, d[0]);
+                    tmem_load32(tmem_row + (it % L::kAcc) * N, d[0]);
                 }
                 // (in three runs, so that looking ahead to the next tile costs the loop itself nothing)
                 int kb = k0;
@@ -729,7 +750,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     const int stop = run == 0 ? max(k0, k1 - 3) : run == 1 ? max(k0, k1 - 1) : k1;
 #pragma unroll 1
                     for (; ok && kb < stop; ++kb) {
-                        const uint32_t b = it & 1;
+                        const uint32_t b = it % L::kAcc;
                         const float s = scale;
                         scale = sx * sw;
                         if (kb + 2 < k1) {
@@ -747,19 +768,18 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                                 tmem_fence_before();
                                 __syncwarp();
                                 if (lane == 0) {
-                                    if constexpr (PAIR) cluster_arrive(lead_acc_empty + 8 * b);
-                                    else mbar_arrive(acc_empty + 8 * b);
+                                    cluster_arrive(lead_acc_empty + 8 * b);
                                 }
-                                if (kb + 1 < k1) next = ask(acc_full + 8 * (it & 1), (it / 2) & 1);
+                                if (kb + 1 < k1) next = test(acc_full + 8 * (it % L::kAcc), (it / L::kAcc) & 1);
                             }
 #pragma unroll
                             for (int i = 0; i < 32; i += 2) fma_pair(acc[c * 32 + i], acc[c * 32 + i + 1], d[c & 1][i], d[c & 1][i + 1], s, s);
                         }
                         if (kb + 1 < k1) {
-                            ok = __all_sync(kFull, next) || warp_wait(acc_full + 8 * (it & 1), (it / 2) & 1);
+                            ok = __all_sync(kFull, next) || warp_wait(acc_full + 8 * (it % L::kAcc), (it / L::kAcc) & 1);
                             if (ok) {
                                 tmem_fence_after();
-                                tmem_load32(tmem_row + (it & 1) * N, d[0]);
+                                tmem_load32(tmem_row + (it % L::kAcc) * N, d[0]);
                             }
                         }
                     }
@@ -847,8 +867,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 }
 #pragma unroll 1
                 for (int kb = k0; kb < k1; ++kb, ++it) {
-                    const uint32_t b = it & 1;
-                    float *scale = scales + b * N;
+                    const uint32_t b = it % L::kAcc;
+                    float *scale = scales + (it & 1) * N;
 #pragma unroll
                     for (int j = 0; j < kOwn; ++j) {
                         if (N % 32 == 0 || lane < N) scale[lane + 32 * j] = sx[j] * sw;
@@ -858,7 +878,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     sw = sw_next;
                     if (kb + 2 < k1) sw_next = __ldg(ws + kb + 2);
                     __syncwarp();
-                    if (!warp_wait(acc_full + 8 * b, (it / 2) & 1)) {
+                    if (!warp_wait(acc_full + 8 * b, (it / L::kAcc) & 1)) {
                         ok = false;
                         break;
                     }
@@ -1026,7 +1046,7 @@ int prepare_fp8(int dev) {
 template <int N, bool PAIR, bool GROUPED>
 int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_rows, const Fp8Args &args, int64_t blocks, cudaStream_t stream) {
     using L = Layout<N, PAIR, GROUPED>;
-    static_assert(L::kStages + 3 < kTileRing, "the producer's lead");
+    static_assert(L::kStages + L::kAcc + 1 < kTileRing, "the producer's lead");
     static_assert(PAIR || 2 * (L::kDynamic + 1024) <= 228 * 1024, "two blocks per multiprocessor");
     static_assert(L::kDynamic <= 227 * 1024, "shared memory of a block");
     CUtensorMap wmap, xmap;
