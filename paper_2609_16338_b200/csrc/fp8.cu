@@ -167,7 +167,8 @@ struct Layout {
     static constexpr int kBRows = PAIR ? N / 2 : N;     // of the B operand in this block's shared memory
     static constexpr uint32_t kBBytes = kBRows * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = PAIR || N == 16 || (N == 32 && !GROUPED) ? 5 : 4;
+    static constexpr int kBlocks = PAIR ? 1 : N == 16 && GROUPED ? 3 : 2;       // per multiprocessor
+    static constexpr int kStages = kBlocks == 3 ? 3 : PAIR || N == 16 || (N == 32 && !GROUPED) ? 5 : 4;
     static constexpr int kParts = PAIR ? 2 : 1;          // of an accumulator's columns, one for every four promoter warps
     static constexpr int kAcc = PAIR ? 2 : 4;            // accumulators in turn
     static constexpr int kColumns = N / kParts;         // per promoter thread
@@ -410,7 +411,7 @@ __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const GroupLists *li
 }
 
 template <int N, bool PAIR, bool GROUPED>
-__global__ void __launch_bounds__(Layout<N, PAIR, GROUPED>::kThreads, PAIR ? 1 : 2)
+__global__ void __launch_bounds__(Layout<N, PAIR, GROUPED>::kThreads, Layout<N, PAIR, GROUPED>::kBlocks)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ Fp8Args a) {
     using L = Layout<N, PAIR, GROUPED>;
     constexpr int kStages = L::kStages;
@@ -1047,7 +1048,7 @@ template <int N, bool PAIR, bool GROUPED>
 int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_rows, const Fp8Args &args, int64_t blocks, cudaStream_t stream) {
     using L = Layout<N, PAIR, GROUPED>;
     static_assert(L::kStages + L::kAcc + 1 < kTileRing, "the producer's lead");
-    static_assert(PAIR || 2 * (L::kDynamic + 1024) <= 228 * 1024, "two blocks per multiprocessor");
+    static_assert(L::kBlocks * (L::kDynamic + 1024) <= 228 * 1024 && L::kBlocks * L::kTmemColumns <= 512, "the blocks of a multiprocessor");
     static_assert(L::kDynamic <= 227 * 1024, "shared memory of a block");
     CUtensorMap wmap, xmap;
     int rc = encode(&wmap, W, K, args.M, experts, PAIR ? L::kBRows : kARows);
@@ -1266,7 +1267,7 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
     // (no more blocks than there can be tiles)
     const int64_t most = [&](int64_t rows) { return (n_pairs / rows + std::min<int64_t>(max_groups, n_pairs)) * a.w_tiles; }(16);
     const int64_t two = std::min<int64_t>(2 * sms, most);
-    if (mean <= 8) return launch_fp8<16, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
+    if (mean <= 8) return launch_fp8<16, false, true>(W, x, K, n_experts, n_xrows, a, std::min<int64_t>(3 * sms, most), stream);
     if (mean <= 16) return launch_fp8<32, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     if (mean <= 32) return launch_fp8<64, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     a.w_tiles = static_cast<int>((M + 255) / 256);
