@@ -123,7 +123,7 @@ struct Fp8Args {
     int w_blocks;               // ceil(M / 128)
     int out_bf16;
     int vector;                 // rows of y may be written 16 bytes at a time
-    int splits;                 // blocks of a cluster, each with its share of K (weights first, dense)
+    int splits;                 // blocks of a cluster, each with its share of K (weights first)
     int row_tiles, w_tiles;     // dense: tiles along the tokens, along the weights (grouped: w_tiles only)
     // grouped
     const int32_t *group_expert, *group_begin, *n_groups, *pair_xrow;
@@ -425,7 +425,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     Tile *ring = reinterpret_cast<Tile *>(smem + L::kTiles);
     GroupLists *lists = reinterpret_cast<GroupLists *>(smem + L::kPrefix);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int splits = GROUPED || PAIR ? 1 : a.splits;
+    const int splits = PAIR ? 1 : a.splits;
     const bool gather = GROUPED && a.pair_xrow != nullptr;
     const int rank = PAIR || splits > 1 ? static_cast<int>(cluster_rank()) : 0;
     const int k_rank = PAIR ? 0 : rank;
@@ -528,6 +528,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
         __syncthreads();
         n_tiles = lists->tiles[n_groups];
+        if (splits > 1) n_tiles = min(n_tiles, t_step);       // (a cluster adds up one tile; the host counted on no more)
     }
     constexpr uint32_t kXBytes = PAIR ? kABytes : L::kBBytes;
     bool ok = true;
@@ -938,14 +939,18 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     }
     if (!ok && a.status) *a.status = 1u;
 
-    if constexpr (!GROUPED && !PAIR) {
+    if constexpr (!PAIR) {
         if (splits > 1) {
             cluster_sync();
-            if (warp >= L::kFirst) {
+            if (warp >= L::kFirst && t_first < n_tiles) {
                 // a warp adds a token's 128 rows, four a lane; the blocks of the cluster share out the tokens
                 const Tile tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t_first, rank);
                 const int64_t m = tile.w0 + lane * 4;
                 for (int n = rank + splits * (warp - L::kFirst); n < tile.rows; n += splits * L::kPromoters) {
+                    if (GROUPED && a.pair_xrow) {            // (a row of x that does not exist: not written)
+                        const int r = __ldg(a.pair_xrow + tile.row0 + n);
+                        if (r < 0 || r >= a.n_xrows) continue;
+                    }
                     float4 part[kMaxSplits];
 #pragma unroll
                     for (int r = 0; r < kMaxSplits; ++r)
@@ -1098,15 +1103,14 @@ int multiprocessors(int *sms) {
 // 16 KB; start, first copies and the cluster's sum cost 2 us more per round.  The clusters that the device holds at once are asked for
 // once per kernel and device (of seven blocks there are 30: 40 row blocks of 5120 x 25600 took two rounds and 36 us).
 constexpr int64_t kGroupNs16 = 270, kGroupNs32 = 310, kGroupNs64 = 490, kRoundNs = 2000, kPairGroupNs = 410, kPairNs = 3500;
-template <int N>
-int plan_weights_first(const Fp8Args &a, int sms, int *splits_out, int64_t *ns_out) {
-    const int64_t tiles = (a.rows + N - 1) / N * a.w_blocks;
+template <int N, bool GROUPED>
+int plan_weights_first(const Fp8Args &a, int64_t tiles, int sms, int *splits_out, int64_t *ns_out) {
     if (tiles > INT_MAX / kMaxSplits) return BITCOS_ERR_SHAPE;
     static int held[32][kMaxSplits + 1];
     int dev = 0;
     int rc = check_cuda(cudaGetDevice(&dev));
     if (rc) return rc;
-    rc = prepare_fp8<N, false, false>(dev);
+    rc = prepare_fp8<N, false, GROUPED>(dev);
     if (rc) return rc;
     constexpr int64_t group_ns = N == 16 ? kGroupNs16 : N == 32 ? kGroupNs32 : kGroupNs64;
     *ns_out = INT64_MAX;
@@ -1116,20 +1120,22 @@ int plan_weights_first(const Fp8Args &a, int sms, int *splits_out, int64_t *ns_o
             cudaLaunchConfig_t cfg{};
             cudaLaunchAttribute attr{};
             cfg.gridDim = dim3(static_cast<unsigned>(splits));
-            cfg.blockDim = dim3(Layout<N, false, false>::kThreads);
-            cfg.dynamicSmemBytes = Layout<N, false, false>::kDynamic;
+            cfg.blockDim = dim3(Layout<N, false, GROUPED>::kThreads);
+            cfg.dynamicSmemBytes = Layout<N, false, GROUPED>::kDynamic;
             attr.id = cudaLaunchAttributeClusterDimension;
             attr.val.clusterDim.x = static_cast<unsigned>(splits);
             attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
             cfg.attrs = &attr;
             cfg.numAttrs = 1;
-            rc = check_cuda(cudaOccupancyMaxActiveClusters(&clusters, fp8_matmul_kernel<N, false, false>, &cfg));
+            rc = check_cuda(cudaOccupancyMaxActiveClusters(&clusters, fp8_matmul_kernel<N, false, GROUPED>, &cfg));
             if (rc) return rc;
-            clusters = 2 * std::max(clusters, 1);      // (it counts one block per multiprocessor, of any size; two are there)
+            clusters = Layout<N, false, GROUPED>::kBlocks * std::max(clusters, 1);      // (it counts one block per multiprocessor, whatever its size)
             if (dev < 32) held[dev][splits] = clusters;
         }
-        const int64_t rounds = (tiles + clusters - 1) / clusters, active = std::min<int64_t>(tiles, clusters) * splits;
-        const int64_t memory_ns = active * 730 / (2 * sms);                   // 16 KB each at 6.5 TB/s
+        const int64_t rounds = (tiles + clusters - 1) / clusters;
+        if (GROUPED && splits > 1 && rounds > 1) continue;                    // (the blocks of a cluster take one tile)
+        const int64_t active = std::min<int64_t>(tiles, clusters) * splits;
+        const int64_t memory_ns = active * 365 / sms;                         // 16 KB each at 6.5 TB/s
         const int64_t ns = rounds * (kRoundNs + (a.G + splits - 1) / splits * std::max(group_ns, memory_ns));
         if (ns < *ns_out) {
             *ns_out = ns;
@@ -1141,9 +1147,9 @@ int plan_weights_first(const Fp8Args &a, int sms, int *splits_out, int64_t *ns_o
 template <int N>
 int launch_weights_first(const void *W, const void *x, int64_t K, Fp8Args &a, int sms, cudaStream_t stream) {
     int64_t ns = 0;
-    const int rc = plan_weights_first<N>(a, sms, &a.splits, &ns);
-    if (rc) return rc;
     const int64_t row_tiles = (a.rows + N - 1) / N;
+    const int rc = plan_weights_first<N, false>(a, row_tiles * a.w_blocks, sms, &a.splits, &ns);
+    if (rc) return rc;
     a.row_tiles = static_cast<int>(row_tiles);
     a.w_tiles = a.w_blocks;
     return launch_fp8<N, false, false>(W, x, K, 1, a.rows, a, row_tiles * a.w_blocks * a.splits, stream);
@@ -1206,7 +1212,7 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
         // few rows: whichever ends sooner
         int splits = 0;
         int64_t ns = 0;
-        rc = plan_weights_first<64>(a, sms, &splits, &ns);
+        rc = plan_weights_first<64, false>(a, (rows + 63) / 64 * a.w_blocks, sms, &splits, &ns);
         if (rc) return rc;
         pairs = kPairNs + (row_tiles * w_tiles + sms / 2 - 1) / (sms / 2) * a.G * kPairGroupNs <= ns;
     }
@@ -1267,7 +1273,14 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
     // (no more blocks than there can be tiles)
     const int64_t most = [&](int64_t rows) { return (n_pairs / rows + std::min<int64_t>(max_groups, n_pairs)) * a.w_tiles; }(16);
     const int64_t two = std::min<int64_t>(2 * sms, most);
-    if (mean <= 8) return launch_fp8<16, false, true>(W, x, K, n_experts, n_xrows, a, std::min<int64_t>(3 * sms, most), stream);
+    if (mean <= 8) {
+        // (a tile per pair at most: with few pairs K is cut as in the dense product)
+        int64_t ns = 0;
+        rc = plan_weights_first<16, true>(a, n_pairs * a.w_blocks, sms, &a.splits, &ns);
+        if (rc) return rc;
+        return launch_fp8<16, false, true>(W, x, K, n_experts, n_xrows, a,
+                                           a.splits > 1 ? n_pairs * a.w_blocks * a.splits : std::min<int64_t>(3 * sms, most), stream);
+    }
     if (mean <= 16) return launch_fp8<32, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     if (mean <= 32) return launch_fp8<64, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     a.w_tiles = static_cast<int>((M + 255) / 256);
