@@ -7,15 +7,20 @@
 //
 // The scales change with every group of 128, so the tensor cores may add up one group only: each group is four
 // tcgen05.mma (K = 32) into a fresh accumulator in tensor memory, and warps of their own ("promoters") read it back, multiply with
-// the two scales and add in fp32 registers while the next group is being multiplied into the other accumulator.
+// the two scales and add in fp32 registers while the next groups are being multiplied into other accumulators.
 //
-// Two operand orders, chosen by the host (choose_dense, choose_grouped):
-//   tokens first   A = 128 tokens, B = 256 weight rows.  A promoter thread holds 64 columns of one token; the scales of a group are
-//                  one number per thread.  Tiles are spread over persistent blocks.  For prompts.
-//   weights first  A = 128 weight rows, B = 16 .. 128 tokens.  The weights pass once for up to 128 tokens, two blocks per
-//                  multiprocessor keep enough of them in flight, and K is cut over the blocks of a cluster where there are few row
-//                  blocks: each leaves its sums in shared memory, and the cluster adds them in order of rank (no workspace, no
-//                  atomics, the same bits every time).  For decoding.
+// Two operand orders, chosen by the host from the sizes:
+//   tokens first   (more than 64 rows, longer groups) A = 256 tokens, B = 256 weight rows, two blocks of a cluster as one
+//                  (cta_group::2): each loads its 128 tokens and half of the weight rows, 64 bytes a clock and multiprocessor from L2 at the
+//                  tensor cores' rate, where a block by itself would need 96 and L2 gives about 40 (11 TB/s).  A promoter thread holds 128
+//                  columns of one token; the scales of a group are one number per thread.  Persistent.  4095 x 8192 x 5120: 147 us
+//                  (2.3 PFLOP/s); a group of 128 takes about 800 clocks for the 512 of its products: what bounds it is the round
+//                  products -> promoters -> products over two accumulators, all that tensor memory holds of 256 columns (and at 2 PFLOP/s and
+//                  more the power limit: the clock is at 1.4 GHz).
+//   weights first  A = 128 weight rows, B = 16, 32 or 64 tokens.  Two or three blocks per multiprocessor keep enough of the weights
+//                  under way, and K is cut over the blocks of a cluster where there are few row blocks: each leaves its sums in shared
+//                  memory, and the cluster adds them in order of rank (no workspace, no atomics, the same bits every time).  Bound by
+//                  memory: 25600 x 5120 at one token 22.6 us (5.8 TB/s).
 //
 // Operands come by TMA (128-byte swizzle, 128 bytes of K per stage); rows of routed pairs by cp.async from two warps of their own.
 #include "bitcos.h"
@@ -136,12 +141,10 @@ struct Tile {
     int w0;                     // first weight row
     int expert;
 };
-// The producer hands the tiles on in a ring.  It is ahead by the stages, the two accumulators and the tile that is being written
-// out at most, less than the ring holds: nobody has to say that an entry has been read.
+// The producer hands the tiles on in a ring.  It is ahead by the stages, the accumulators and the tile that is being written out at
+// most, less than the ring holds: nobody has to say that an entry has been read.
 constexpr int kTileRing = 16;
 
-// PAIR (tokens first, dense): two blocks of a cluster multiply as one, 256 tokens by 256 weight rows; each loads its own 128
-// tokens and half of the weight rows.
 // A place in the ring of stages and the parity of its round.  (Counted along: a remainder and a quotient at every step are 50 clocks of
 // a warp that has about 500 for one.)
 template <int STAGES>
@@ -162,6 +165,7 @@ struct GroupLists {
     int32_t expert[kMaxGroups];
 };
 
+// N columns of an accumulator; PAIR: tokens first; GROUPED: over routed pairs.
 template <int N, bool PAIR, bool GROUPED>
 struct Layout {
     static constexpr int kBRows = PAIR ? N / 2 : N;     // of the B operand in this block's shared memory
@@ -947,8 +951,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 const Tile tile = find_tile<N, PAIR, GROUPED>(a, lists, n_groups, t_first, rank);
                 const int64_t m = tile.w0 + lane * 4;
                 for (int n = rank + splits * (warp - L::kFirst); n < tile.rows; n += splits * L::kPromoters) {
-                    if (GROUPED && a.pair_xrow) {            // (a row of x that does not exist: not written)
-                        const int r = __ldg(a.pair_xrow + tile.row0 + n);
+                    if (GROUPED) {                           // (a row of x that does not exist: not written)
+                        const int64_t r = a.pair_xrow ? __ldg(a.pair_xrow + tile.row0 + n) : tile.row0 + n;
                         if (r < 0 || r >= a.n_xrows) continue;
                     }
                     float4 part[kMaxSplits];
@@ -1105,7 +1109,8 @@ int multiprocessors(int *sms) {
 constexpr int64_t kGroupNs16 = 270, kGroupNs32 = 310, kGroupNs64 = 490, kRoundNs = 2000, kPairGroupNs = 410, kPairNs = 3500;
 template <int N, bool GROUPED>
 int plan_weights_first(const Fp8Args &a, int64_t tiles, int sms, int *splits_out, int64_t *ns_out) {
-    if (tiles > INT_MAX / kMaxSplits) return BITCOS_ERR_SHAPE;
+    *splits_out = 1;
+    if (tiles > INT_MAX / kMaxSplits) return GROUPED ? BITCOS_OK : BITCOS_ERR_SHAPE;
     static int held[32][kMaxSplits + 1];
     int dev = 0;
     int rc = check_cuda(cudaGetDevice(&dev));

@@ -202,11 +202,11 @@ def test_grouped(bc, tokens, top_k, experts, M, K, out):
     assert torch.equal(y, z)
 
 
-@pytest.mark.parametrize("tokens,top_k,experts", [(24, 4, 12), (600, 4, 12)])
-def test_grouped_malformed_lists_are_skipped(bc, tokens, top_k, experts):
+@pytest.mark.parametrize("tokens,top_k,experts,K", [(24, 4, 12, 256), (600, 4, 12, 256), (5, 7, 12, 1024), (100, 6, 12, 128)])
+def test_grouped_malformed_lists_are_skipped(bc, tokens, top_k, experts, K):
     """A group that names no expert, one that ends behind the pairs, one that begins below them, one pair whose row does not exist, an
     empty group in between, more groups than there is room for: nothing of the bad ones is written, the rest is as it was."""
-    M, K = 384, 256
+    M = 384
     w, ws = weights(experts, M, K, 9)
     x, xs = activations(tokens, K, 9)
     (ge, gb, ng, xr), groups = routed(tokens, top_k, experts, 9)
