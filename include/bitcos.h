@@ -679,8 +679,9 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
  *   x        device bytes [n_xrows][K];  x_scale   device float [n_xrows][K/128];  y   device [n_pairs][M]
  * The lists are checked on the device: a group whose expert is outside [0, n_experts) or whose pairs lie outside [0, n_pairs) is
  * skipped whole, a pair whose row is outside [0, n_xrows) alone; nothing of them is written and the status word is set
- * to 2.  An empty group is skipped without a mark.  Rows of y that no group covers are left as they were.  W is read after every
- * earlier kernel in the stream has completed.  Everything else as for bitcos_fp8_matmul. */
+ * to 2.  An empty group is skipped without a mark.  Groups do not overlap (which of two writes a row that both cover is not said).
+ * Rows of y that no group covers are left as they were.  W is read after every earlier kernel in the stream has completed.
+ * Everything else as for bitcos_fp8_matmul. */
 int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_experts, int64_t M, int64_t K, const int32_t *group_expert,
                               const int32_t *group_begin, const int32_t *n_groups_device, int max_groups, const int32_t *pair_xrow,
                               int64_t n_pairs, const uint8_t *x, const float *x_scale, int64_t n_xrows, void *y, int y_type, void *workspace,

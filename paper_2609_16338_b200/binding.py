@@ -1105,10 +1105,9 @@ def bitcos_fp8_matmul_grouped(W: Fp8Weights, group_expert, group_begin, n_groups
     _require(W.experts is not None, "W must hold experts ([experts, M, K])")
     for t in (group_expert, group_begin, n_groups, pair_xrow):
         _require(t is None or (t.dtype == torch.int32 and t.is_contiguous()), "the lists must be contiguous int32 tensors")
-    if pair_xrow is not None:
-        n_pairs = pair_xrow.numel()
-    elif n_pairs is None:
-        n_pairs = x.shape[0]
+    if n_pairs is None:
+        n_pairs = x.shape[0] if pair_xrow is None else pair_xrow.numel()
+    _require(pair_xrow is None or pair_xrow.numel() == n_pairs, "pair_xrow must have n_pairs entries")
     max_groups = group_expert.numel()
     _require(group_begin.numel() > max_groups and n_groups.numel() >= 1, "group_begin must have one entry more than group_expert")
     y, code = _fp8_operands(W, x, x_scale, n_pairs, y, out_dtype, workspace)

@@ -532,7 +532,10 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
         __syncthreads();
         n_tiles = lists->tiles[n_groups];
-        if (splits > 1) n_tiles = min(n_tiles, t_step);       // (a cluster adds up one tile; the host counted on no more)
+        if (splits > 1 && n_tiles > t_step) {                // (a cluster adds up one tile; groups that do not overlap have no more)
+            n_tiles = t_step;
+            if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = 2u;
+        }
     }
     constexpr uint32_t kXBytes = PAIR ? kABytes : L::kBBytes;
     bool ok = true;
