@@ -13,7 +13,7 @@
 //   tokens first   (more than 64 rows, longer groups) A = 256 tokens, B = 256 weight rows, two blocks of a cluster as one
 //                  (cta_group::2): each loads its 128 tokens and half of the weight rows, 64 bytes a clock and multiprocessor from L2 at the
 //                  tensor cores' rate, where a block by itself would need 96 and L2 gives about 40 (11 TB/s).  A promoter thread holds 128
-//                  columns of one token; the scales of a group are one number per thread.  Persistent.  4095 x 8192 x 5120: 147 us
+//                  columns of one token; the scales of a group are one number per thread.  Persistent.  4095 x 8192 x 5120: 146 to 152 us
 //                  (2.3 PFLOP/s); a group of 128 takes about 800 clocks for the 512 of its products: what bounds it is the round
 //                  products -> promoters -> products over two accumulators, all that tensor memory holds of 256 columns (and at 2 PFLOP/s and
 //                  more the power limit: the clock is at 1.4 GHz).
@@ -172,7 +172,8 @@ struct Layout {
     static constexpr uint32_t kBBytes = kBRows * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
     static constexpr int kBlocks = PAIR ? 1 : N == 16 && GROUPED ? 3 : 2;       // per multiprocessor
-    static constexpr int kStages = kBlocks == 3 ? 3 : PAIR || N == 16 || (N == 32 && !GROUPED) ? 5 : 4;
+    // (PAIR: four stages leave room for the outputs; a fifth changed no time by more than 0.5 %)
+    static constexpr int kStages = kBlocks == 3 ? 3 : N == 16 || (N == 32 && !GROUPED) ? 5 : 4;
     static constexpr int kParts = PAIR ? 2 : 1;          // of an accumulator's columns, one for every four promoter warps
     static constexpr int kAcc = PAIR ? 2 : 4;            // accumulators in turn
     static constexpr int kColumns = N / kParts;         // per promoter thread
@@ -184,14 +185,15 @@ struct Layout {
     static constexpr int kWRowsPerTile = PAIR ? N : kARows;
     static constexpr uint32_t kTmemColumns = kAcc * N;
     // byte offsets behind the stages
-    static constexpr uint32_t kBars = kStages * kStageBytes;
+    // PAIR: two boxes of 32 rows of 128 bytes per promoter warp, swizzled as TMA wants them, from which the outputs go to memory
+    static constexpr uint32_t kOutBox = 32 * 128, kOutBoxes = 2;
+    static constexpr uint32_t kOut = kStages * kStageBytes;
+    static constexpr uint32_t kBars = kOut + (PAIR ? kPromoters * kOutBoxes * kOutBox : 0);
     static constexpr uint32_t kTiles = kBars + (3 * kStages + 2 * kAcc + 1 + kTileRing) * 8;
     static constexpr uint32_t kRows = kTiles + kTileRing * sizeof(Tile);
     static constexpr uint32_t kTmem = kRows + (GROUPED ? 2 * kRowsPerTile * 4 : 0);
     static constexpr uint32_t kScales = (kTmem + 4 + 15) / 16 * 16;
-    // PAIR: 32 rows of 128 bytes and 16 of padding per promoter warp, through which the outputs go to memory by whole lines
-    static constexpr uint32_t kOutPitch = 144, kOutBytes = 32 * kOutPitch;
-    static constexpr uint32_t kPrefix = kScales + (PAIR ? kPromoters * kOutBytes : kPromoters * 2 * N * 4);
+    static constexpr uint32_t kPrefix = kScales + (PAIR ? 0 : kPromoters * 2 * N * 4);
     static constexpr uint32_t kTotal = kPrefix + (GROUPED ? sizeof(GroupLists) : 0);
     static constexpr uint32_t kDynamic = kTotal + 1024;  // (the stages start on a 1024-byte boundary)
 };
@@ -216,6 +218,10 @@ __device__ __forceinline__ void tma_3d_pair(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
                  "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
                  : "memory");
+}
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int c0, int c1, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c0), "r"(c1), "r"(src) : "memory");
 }
 
 // 16 bytes from anywhere in global memory, asynchronously; with there = 0 nothing is read and zeros are written.  (The rows of routed
@@ -416,7 +422,8 @@ __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const GroupLists *li
 
 template <int N, bool PAIR, bool GROUPED>
 __global__ void __launch_bounds__(Layout<N, PAIR, GROUPED>::kThreads, Layout<N, PAIR, GROUPED>::kBlocks)
-fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ Fp8Args a) {
+fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap,
+                  const __grid_constant__ Fp8Args a) {
     using L = Layout<N, PAIR, GROUPED>;
     constexpr int kStages = L::kStages;
     extern __shared__ uint8_t smem_raw[];
@@ -797,55 +804,87 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 }
                 if (!ok) break;
                 const int64_t c0 = tile.w0 + part * kCols;
-                // A thread has a row, memory wants lines: each warp turns its 32 rows round in shared memory, 128 bytes of a row
-                // at a time.  (Straight from the registers, 32 rows an instruction and half a sector each, a tile took 5 us.)
+                // A thread has a row, memory wants lines: each warp puts its 32 rows into shared memory, two boxes of 128 bytes of a row at
+                // a time, and TMA writes them while the next tile's groups are added.  (Stored by the warp itself, line by line, a tile
+                // waited 1.2 us for its 64 KB; straight from the registers, 32 rows an instruction and half a sector each, 5 us.)  Where not all 32 rows
+                // are the tile's (dense: behind the last one TMA writes nothing), or rows are not whole 16 bytes, the warp does it.
                 const uint32_t rows_mask = __ballot_sync(kFull, mine);
-                uint8_t *out = smem + L::kScales + (warp - L::kFirst) * L::kOutBytes;
-                const auto flush = [&](int from, int width) {           // columns from .. + width: 128 bytes
+                const int64_t first = tile.row0 + quarter * 32;
+                uint8_t *out = smem + L::kOut + (warp - L::kFirst) * L::kOutBoxes * L::kOutBox;
+                const bool bulk = a.vector && (rows_mask == kFull || (!GROUPED && rows_mask));
+                const int size = a.out_bf16 ? 2 : 4, width = 128 / size;         // bytes of an output, columns of a box
+                const auto boxes_free = [&]() {                        // TMA has read the last ones
+                    if (elect_one()) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     __syncwarp();
-                    const int64_t first = tile.row0 + quarter * 32;
-                    const int left = static_cast<int>(min(static_cast<int64_t>(width), a.M - c0 - from)), size = 128 / width;
-                    if (a.vector) {
-                        const int at = (lane & 7) * (width / 8);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int r = (lane >> 3) + 4 * j;
-                            const uint4 v = *reinterpret_cast<const uint4 *>(out + r * L::kOutPitch + (lane & 7) * 16);
-                            if (((rows_mask >> r) & 1u) && at < left)
-                                *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.y) + ((first + r) * a.M + c0 + from + at) * size) = v;
+                };
+                const auto put = [&](int box, int i, uint4 v) {        // 16 bytes i of this thread's row
+                    *reinterpret_cast<uint4 *>(out + box * L::kOutBox + lane * 128 + ((i ^ (lane & 7)) << 4)) = v;
+                };
+                const auto send = [&](int from) {                      // columns from .. + 2 * width
+                    if (bulk) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (elect_one()) {
+                            for (int box = 0; box < static_cast<int>(L::kOutBoxes); ++box)
+                                if (c0 + from + box * width < a.M)
+                                    tma_store_2d(&ymap, static_cast<int>(c0) + from + box * width, static_cast<int>(first), smem_addr(out + box * L::kOutBox));
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                         }
-                    } else {
-                        for (int r = 0; r < 32; ++r)
-                            if ((rows_mask >> r) & 1u)
-                                for (int i = lane; i < left; i += 32) {
-                                    const int64_t to = (first + r) * a.M + c0 + from + i;
-                                    if (size == 2)
-                                        static_cast<uint16_t *>(a.y)[to] = *reinterpret_cast<const uint16_t *>(out + r * L::kOutPitch + i * 2);
-                                    else static_cast<uint32_t *>(a.y)[to] = *reinterpret_cast<const uint32_t *>(out + r * L::kOutPitch + i * 4);
-                                }
+                        __syncwarp();
+                        return;
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int box = 0; box < static_cast<int>(L::kOutBoxes); ++box) {
+                        const uint8_t *o = out + box * L::kOutBox;
+                        const int64_t column = c0 + from + box * width;
+                        const int left = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(width), a.M - column)));
+                        if (a.vector) {
+                            const int at = (lane & 7) * (width / 8);
+                            uint8_t *to = static_cast<uint8_t *>(a.y) + ((first + (lane >> 3)) * a.M + column + at) * size;
+                            const int64_t step = 4 * a.M * size;
+                            const uint8_t *from_even = o + (lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4);
+                            const uint8_t *from_odd = o + ((lane >> 3) + 4) * 128 + (((lane & 7) ^ ((lane >> 3) + 4)) << 4);
+                            const uint32_t mask = at < left ? rows_mask >> (lane >> 3) : 0u;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const uint4 v = *reinterpret_cast<const uint4 *>((j & 1 ? from_odd : from_even) + (j / 2) * 1024);
+                                if ((mask >> (4 * j)) & 1u) *reinterpret_cast<uint4 *>(to) = v;
+                                to += step;
+                            }
+                        } else {
+                            for (int r = 0; r < 32; ++r)
+                                if ((rows_mask >> r) & 1u)
+                                    for (int i = lane; i < left; i += 32) {
+                                        const int64_t to = (first + r) * a.M + column + i;
+                                        const uint8_t *v = o + r * 128 + ((i * size) ^ ((r & 7) << 4));
+                                        if (size == 2) static_cast<uint16_t *>(a.y)[to] = *reinterpret_cast<const uint16_t *>(v);
+                                        else static_cast<uint32_t *>(a.y)[to] = *reinterpret_cast<const uint32_t *>(v);
+                                    }
+                        }
                     }
                     __syncwarp();
                 };
-                uint4 *mine_out = reinterpret_cast<uint4 *>(out + lane * L::kOutPitch);
-                if (a.out_bf16) {
+                if (rows_mask) {
+                    if (a.out_bf16) {
+                        boxes_free();
 #pragma unroll
-                    for (int c = 0; c < kCols; c += 64) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float *v = acc + c + i * 8;
-                            mine_out[i] = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+                        for (int i = 0; i < 16; ++i) {
+                            const float *v = acc + i * 8;
+                            put(i / 8, i % 8, make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])));
                         }
-                        flush(c, 64);
-                    }
-                } else {
+                        send(0);
+                    } else {
 #pragma unroll
-                    for (int c = 0; c < kCols; c += 32) {
+                        for (int c = 0; c < kCols; c += 64) {
+                            boxes_free();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float *v = acc + c + i * 4;
-                            mine_out[i] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                            for (int i = 0; i < 16; ++i) {
+                                const float *v = acc + c + i * 4;
+                                put(i / 8, i % 8, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+                            }
+                            send(c);
                         }
-                        flush(c, 32);
                     }
                 }
             } else {
@@ -945,6 +984,10 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
     }
     if (!ok && a.status) *a.status = 1u;
+    if constexpr (PAIR) {                  // (the outputs are in memory before the block goes)
+        if (warp >= L::kFirst && elect_one()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
+    }
 
     if constexpr (!PAIR) {
         if (splits > 1) {
@@ -1032,6 +1075,22 @@ int encode(CUtensorMap *map, const void *data, int64_t K, int64_t rows, int expe
     return BITCOS_OK;
 }
 
+// The outputs: boxes of 32 rows of 128 bytes.
+int encode_outputs(CUtensorMap *map, const Fp8Args &a) {
+    const EncodeTiled f = encode_tiled();
+    const cuuint64_t size = a.out_bf16 ? 2 : 4;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.M), static_cast<cuuint64_t>(a.rows)}, strides[1] = {static_cast<cuuint64_t>(a.M) * size};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / size), 32}, ones[2] = {1, 1};
+    const CUresult r = f(map, a.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, a.y, dims, strides, box, ones,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        g_last_cuda_error = cudaErrorInvalidValue;
+        return BITCOS_ERR_CUDA;
+    }
+    return BITCOS_OK;
+}
+
 // Once per kernel and device, as in prepare_kernel, and all of the cache as shared memory.
 template <int N, bool PAIR, bool GROUPED>
 int prepare_fp8(int dev) {
@@ -1062,10 +1121,12 @@ int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_r
     static_assert(L::kStages + L::kAcc + 1 < kTileRing, "the producer's lead");
     static_assert(L::kBlocks * (L::kDynamic + 1024) <= 228 * 1024 && L::kBlocks * L::kTmemColumns <= 512, "the blocks of a multiprocessor");
     static_assert(L::kDynamic <= 227 * 1024, "shared memory of a block");
-    CUtensorMap wmap, xmap;
+    CUtensorMap wmap, xmap, ymap{};
     int rc = encode(&wmap, W, K, args.M, experts, PAIR ? L::kBRows : kARows);
     if (rc) return rc;
     rc = encode(&xmap, x, K, x_rows, 0, L::kRowsPerTile);
+    if (rc) return rc;
+    if (PAIR && args.vector) rc = encode_outputs(&ymap, args);
     if (rc) return rc;
     auto *kernel = fp8_matmul_kernel<N, PAIR, GROUPED>;
     int dev = 0;
@@ -1087,7 +1148,7 @@ int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_r
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = cluster > 1 ? attr : attr + 1;
     cfg.numAttrs = (cluster > 1 ? 1 : 0) + ((env && env[0] == '0') ? 0 : 1);
-    void *pointers[] = {&wmap, &xmap, const_cast<Fp8Args *>(&args)};
+    void *pointers[] = {&wmap, &xmap, &ymap, const_cast<Fp8Args *>(&args)};
     return check_cuda(cudaLaunchKernelExC(&cfg, reinterpret_cast<const void *>(kernel), pointers));
 }
 
