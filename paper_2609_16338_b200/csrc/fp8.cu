@@ -17,7 +17,7 @@
 //                  (2.3 PFLOP/s); a group of 128 takes about 800 clocks for the 512 of its products: what bounds it is the round
 //                  products -> promoters -> products over two accumulators, all that tensor memory holds of 256 columns (and at 2 PFLOP/s and
 //                  more the power limit: the clock is at 1.4 GHz).
-//   weights first  A = 128 weight rows, B = 16, 32 or 64 tokens.  Two or three blocks per multiprocessor keep enough of the weights
+//   weights first  A = 128 weight rows, B = 16, 32 or 64 tokens (16 of routed pairs).  Two or three blocks per multiprocessor keep enough of the weights
 //                  under way, and K is cut over the blocks of a cluster where there are few row blocks: each leaves its sums in shared
 //                  memory, and the cluster adds them in order of rank (no workspace, no atomics, the same bits every time).  Bound by
 //                  memory: 25600 x 5120 at one token 22.6 us (5.8 TB/s).
@@ -171,9 +171,9 @@ struct Layout {
     static constexpr int kBRows = PAIR ? N / 2 : N;     // of the B operand in this block's shared memory
     static constexpr uint32_t kBBytes = kBRows * kGroup;
     static constexpr uint32_t kStageBytes = kABytes + kBBytes;
-    static constexpr int kBlocks = PAIR ? 1 : N == 16 && GROUPED ? 3 : 2;       // per multiprocessor
+    static constexpr int kBlocks = PAIR ? 1 : GROUPED ? 3 : 2;       // per multiprocessor
     // (PAIR: four stages leave room for the outputs; a fifth changed no time by more than 0.5 %)
-    static constexpr int kStages = kBlocks == 3 ? 3 : N == 16 || (N == 32 && !GROUPED) ? 5 : 4;
+    static constexpr int kStages = kBlocks == 3 ? 3 : N <= 32 ? 5 : 4;
     static constexpr int kParts = PAIR ? 2 : 1;          // of an accumulator's columns, one for every four promoter warps
     static constexpr int kAcc = PAIR ? 2 : 4;            // accumulators in turn
     static constexpr int kColumns = N / kParts;         // per promoter thread
@@ -931,33 +931,27 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                         break;
                     }
                     tmem_fence_after();
-                    // as many columns at once as the registers hold (all of them but in the grouped kernel of 64 tokens), so that the
-                    // accumulator goes back before they are added
-                    constexpr int kWide = kCols < 32 ? 16 : 32, kLoads = GROUPED || kCols <= kWide ? 1 : kCols / kWide;
+                    // all columns at once, so that the accumulator goes back before they are added
+                    constexpr int kWide = kCols < 32 ? 16 : 32, kLoads = kCols / kWide;
+                    uint32_t d[kLoads][kWide];
 #pragma unroll
-                    for (int from = 0; from < kCols; from += kWide * kLoads) {
-                        uint32_t d[kLoads][kWide];
+                    for (int c = 0; c < kLoads; ++c) {
+                        if constexpr (kWide == 16) tmem_load16(tmem_row + b * N + c * kWide, d[c]);
+                        else tmem_load32(tmem_row + b * N + c * kWide, d[c]);
+                    }
 #pragma unroll
-                        for (int c = 0; c < kLoads; ++c) {
-                            if constexpr (kWide == 16) tmem_load16(tmem_row + b * N + from + c * kWide, d[c]);
-                            else tmem_load32(tmem_row + b * N + from + c * kWide, d[c]);
-                        }
+                    for (int c = 0; c < kLoads; ++c) {
+                        if constexpr (kWide == 16) tmem_wait16(d[c]);
+                        else tmem_wait32(d[c]);
+                    }
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(acc_empty + 8 * b);
 #pragma unroll
-                        for (int c = 0; c < kLoads; ++c) {
-                            if constexpr (kWide == 16) tmem_wait16(d[c]);
-                            else tmem_wait32(d[c]);
-                        }
-                        if (from + kWide * kLoads == kCols) {
-                            tmem_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(acc_empty + 8 * b);
-                        }
-#pragma unroll
-                        for (int i = 0; i < kWide * kLoads; i += 4) {
-                            const float4 sc = *reinterpret_cast<const float4 *>(scale + from + i);
-                            fma_pair(acc[from + i], acc[from + i + 1], d[i / kWide][i % kWide], d[i / kWide][i % kWide + 1], sc.x, sc.y);
-                            fma_pair(acc[from + i + 2], acc[from + i + 3], d[i / kWide][i % kWide + 2], d[i / kWide][i % kWide + 3], sc.z, sc.w);
-                        }
+                    for (int i = 0; i < kCols; i += 4) {
+                        const float4 sc = *reinterpret_cast<const float4 *>(scale + i);
+                        fma_pair(acc[i], acc[i + 1], d[i / kWide][i % kWide], d[i / kWide][i % kWide + 1], sc.x, sc.y);
+                        fma_pair(acc[i + 2], acc[i + 3], d[i / kWide][i % kWide + 2], d[i / kWide][i % kWide + 3], sc.z, sc.w);
                     }
                 }
                 if (!ok) break;
@@ -1291,6 +1285,8 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
         a.w_tiles = static_cast<int>(w_tiles);
         return launch_fp8<256, true, false>(W, x, K, 1, rows, a, 2 * std::min<int64_t>(row_tiles * w_tiles, sms / 2), stream);
     }
+    // (the narrowest tile that takes all rows: 25600 x 5120 at 32 rows 25.0 us, with two tiles of 16 35.2; at 64 rows 29.6, with tiles of 32
+    // 38.6, of 16 46.5; 6912 x 2560 at 16 rows 6.55, with a tile of 32 6.74)
     if (rows <= 16) return launch_weights_first<16>(W, x, K, a, sms, stream);
     if (rows <= 32) return launch_weights_first<32>(W, x, K, a, sms, stream);
     return launch_weights_first<64>(W, x, K, a, sms, stream);
@@ -1339,19 +1335,19 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
     const int64_t mean = (n_pairs + max_groups - 1) / max_groups;
     a.w_tiles = a.w_blocks;
     if ((n_pairs / 16 + max_groups) * a.w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
-    // (no more blocks than there can be tiles)
-    const int64_t most = [&](int64_t rows) { return (n_pairs / rows + std::min<int64_t>(max_groups, n_pairs)) * a.w_tiles; }(16);
-    const int64_t two = std::min<int64_t>(2 * sms, most);
-    if (mean <= 8) {
-        // (a tile per pair at most: with few pairs K is cut as in the dense product)
+    // 16 tokens a tile, weights first, against 256, tokens first: 128 experts of 1536 x 2048 (2048 x 768), mean 16 75 us against 123 (39 against
+    // 77), 38 109 against 132 (62 against 75), 48 129 against 131 (76 against 75), 64 165 against 132 (93 against 74).  Tiles of 32 and 64 tokens
+    // lay between: 32 gained 5 to 7 % at means of 20 to 32 on the first shape and lost as much on the second, 64 won 5 % at 48 and nowhere else;
+    // and tiles of 16 cost what the groups' lengths are, whatever their mean.
+    if (mean <= 48) {
+        // (no more blocks than there can be tiles; a tile per pair at most: with few pairs K is cut as in the dense product)
         int64_t ns = 0;
         rc = plan_weights_first<16, true>(a, n_pairs * a.w_blocks, sms, &a.splits, &ns);
         if (rc) return rc;
+        const int64_t most = (n_pairs / 16 + std::min<int64_t>(max_groups, n_pairs)) * a.w_tiles;
         return launch_fp8<16, false, true>(W, x, K, n_experts, n_xrows, a,
                                            a.splits > 1 ? n_pairs * a.w_blocks * a.splits : std::min<int64_t>(3 * sms, most), stream);
     }
-    if (mean <= 16) return launch_fp8<32, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
-    if (mean <= 32) return launch_fp8<64, false, true>(W, x, K, n_experts, n_xrows, a, two, stream);
     a.w_tiles = static_cast<int>((M + 255) / 256);
     return launch_fp8<256, true, true>(W, x, K, n_experts, n_xrows, a, sms / 2 * 2, stream);
 }
