@@ -501,13 +501,13 @@ int launch_route_type(RouteArgs a, cudaStream_t stream) {
 // knows what lies in front of its own (all experts before, the same expert's pairs in earlier chunks), counts its runs, and its
 // warps place their runs 32 pairs at a time (match_any: the earlier lanes with the same expert).
 // ---------------------------------------------------------------------------------------------
-// What bounds it is the chain of passes (count, join, place), each a few dependent reads of memory and shared memory: 13 us for
-// 262144 pairs of 128 experts, where reading and writing them once takes 0.6 us; 2.3 us for 128 pairs.  Recorded in a graph:
+// What bounds it is the chain of passes (count, join, place), each a few dependent reads of memory and shared memory: 11.1 us for
+// 262144 pairs of 128 experts, where reading and writing them once takes 0.6 us; 2.3 us for 128 pairs.  Recorded in a graph, with the
+// threads that a call gets below:
 //   pairs (experts)         1600 (64)  4096 (128)  8192 (128)  32768 (128)  262144 (128)
 //   1024 pairs a chunk      6.2        9.2         8.9         10.1         12.8       (one block up to 4096 pairs)
-//   256 pairs a chunk       4.8        5.0         5.6          9.7         13.2       (one block up to 512 pairs)
-// Past 148 * 256 pairs the chunks grow instead, one block to a multiprocessor.  Blocks of 512 threads are faster for 32768
-// pairs (7.7 against 10.1) and slower for 262144 (17.6 against 12.9).
+//   256 pairs a chunk       4.9        4.9         5.2          7.8         11.1       (one block up to 512 pairs)
+// Past 148 * 256 pairs the chunks grow instead, one block to a multiprocessor.
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortMaxBlocks = 148;
@@ -620,7 +620,8 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
         }
         __syncthreads();
         int all_pairs = 0, all_groups = 0;
-        for (int w = 0; w < warps; ++w) {
+        const int busy = smaller(warps, (E - base + 31) / 32);             // the warps with experts
+        for (int w = 0; w < busy; ++w) {
             if (w == warp) {
                 p += all_pairs;
                 g += all_groups;
@@ -862,15 +863,19 @@ int bitcos_group_pairs_slots(const int32_t *pair_expert, int64_t n_pairs, int to
                static_cast<int>(n_pairs), n_experts, top_k, 0};
     const int blocks = sort_blocks(n_pairs);
     a.chunk = static_cast<int>(((n_pairs + blocks - 1) / blocks + 31) / 32 * 32);
-    // threads: a warp for every 32 pairs of a chunk, but enough of them for the experts
-    int64_t threads = std::max<int64_t>((n_experts + 31) / 32 * 32, a.chunk);
+    // threads: a warp for every 32 pairs of a chunk, but enough of them for the experts and for the blocks' counts, 32 a thread
+    // (32768 pairs of 128 experts: 8.2 us with 512 threads, 12.8 with 256; of 256 experts 10.1 with 1024, 20 with 256)
+    const int64_t counts = blocks > 1 ? (static_cast<int64_t>(blocks) * n_experts / 32 + 31) / 32 * 32 : 128;
+    int64_t threads = std::max<int64_t>({(n_experts + 31) / 32 * 32, a.chunk, counts});
     threads = std::min<int64_t>(kSortThreads, std::max<int64_t>(threads, 128));
     const size_t smem = (threads / 32 + 2) * static_cast<size_t>(n_experts) * sizeof(int32_t);
     int sms = 0, budget = 0;
     int rc = prepare_kernel<place_kernel>(&sms, &budget);
     if (rc) return rc;
     if (blocks > 1) {
-        rc = launch_pdl(count_kernel, dim3(static_cast<unsigned>(blocks)), kSortThreads, n_experts * sizeof(int32_t), stream, a);
+        // (four pairs a thread: 262144 pairs 12.7 us with 256 threads, 13.2 with 1024; a million of 1000 experts 35.3 and 34.3)
+        const int counting = static_cast<int>(std::min<int64_t>(kSortThreads, std::max<int64_t>(256, (a.chunk / 4 + 31) / 32 * 32)));
+        rc = launch_pdl(count_kernel, dim3(static_cast<unsigned>(blocks)), counting, n_experts * sizeof(int32_t), stream, a);
         if (rc) return rc;
     }
     return launch_pdl(place_kernel, dim3(static_cast<unsigned>(blocks)), static_cast<int>(threads), smem, stream, a);
