@@ -10,6 +10,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+from test_gpu_experts import check_route  # noqa: E402
 from test_gpu_fp8 import activations, bc, check, product_reference, weights  # noqa: E402,F401
 
 
@@ -224,3 +225,23 @@ def test_one_row_for_every_place(bc):
     want[7] = 0
     bound = (weight.double().sum(1, keepdim=True) * y[1].double().abs()) * 7 * 2.0 ** -24 + 1e-40
     assert ((out.double() - want).abs() <= bound).all() and (out[7] == 0).all()
+
+
+@pytest.mark.parametrize("experts,n_groups,top_groups", [(256, 8, 4), (1024, 32, 7), (64, 16, 3), (512, 4, 1), (32, 32, 9)])
+@pytest.mark.parametrize("group_best", [1, 2])
+def test_groups_that_32_bits_cannot_tell(bc, experts, n_groups, top_groups, group_best):
+    """Group values that differ by less than a rounding of 32 bits, with and without ties inside the groups, masked experts, groups
+    with one expert left or none: 64 bits decide."""
+    if group_best > experts // n_groups:
+        pytest.skip("a group has one expert")
+    rng = np.random.default_rng(experts + group_best)
+    z = (rng.normal(0, 1e-6, (120, experts)) - 3.0).astype(np.float32)
+    z[40:80] += rng.normal(0, 1, (40, experts)).astype(np.float32) * (rng.random((40, experts)) < 0.9)
+    z[60:100][rng.random((40, experts)) < 0.6] = -np.inf
+    z[100:, ::2] = np.nan
+    bias = (1.0 + rng.integers(-3, 4, experts) * 2.0 ** -23).astype(np.float32)
+    logits = torch.from_numpy(z).cuda()
+    for score in ("sigmoid", "softmax"):
+        check_route(bc, logits, bias, top_k=min(8, experts), score=score, n_groups=n_groups, top_groups=top_groups, group_best=group_best)
+        check_route(bc, logits, None, top_k=min(8, experts), score=score, n_groups=n_groups, top_groups=top_groups, group_best=group_best)
+    check_route(bc, logits.to(torch.bfloat16), bias, top_k=4, score="sigmoid", n_groups=n_groups, top_groups=top_groups, group_best=group_best)
