@@ -28,6 +28,11 @@ constexpr uint32_t kFull = 0xFFFFFFFFu;
 // the order of the scores is the order of the logits, and that is what is compared.  Otherwise c is formed in 32 bits with
 // a bound on its error; where two choices whose order matters lie closer than that allows, the warp does the
 // token once more in 64 bits (route_exact).
+//
+// A warp to a token, so that a place is one reduction over the lanes' first keys and nothing passes through shared memory.  Bound by
+// issue slots (1100 warp instructions a token of 256 experts) and, at the end, by the last tokens that need 64 bits (candidates 2 us, a whole
+// token 10 us): 16384 tokens of 256 experts in 8 groups, bf16, 30 us, 18.7 without such tokens; of 128 experts without groups, fp32, 11 us; one token
+// 2.5 us.  Two or eight warps a block are no faster.
 // ---------------------------------------------------------------------------------------------
 constexpr int kRouteWarps = 4;
 constexpr int kMaxRouteGroups = 32;
