@@ -23,7 +23,13 @@ static int take(PyObject *const *args, Py_ssize_t n, Py_ssize_t want, const char
 }
 
 #define P(i) ((void *)(uintptr_t)v[i])
-#define I(i) ((int)v[i])
+/* (a number that 32 bits do not hold is refused, not cut: 2^32 + 1 groups are not one group) */
+static int narrow(int64_t v, int *wide) {
+    *wide |= v != (int32_t)v;
+    return (int)v;
+}
+static void look_at(int first, ...) { (void)first; }       /* evaluates its arguments */
+#define I(i) narrow(v[i], &wide)
 #define Z(i) ((size_t)v[i])
 #define L(i) (v[i])
 static float as_float(int64_t bits) {
@@ -38,11 +44,16 @@ static float as_float(int64_t bits) {
     static int (*p_##name)(types);                                                          \
     static PyObject *name(PyObject *self, PyObject *const *args, Py_ssize_t n) {            \
         int64_t v[count];                                                                   \
-        int status;                                                                         \
+        int status, wide = 0;                                                               \
         (void)self;                                                                         \
         if (take(args, n, count, #name, v)) return NULL;                                    \
         if (!p_##name) {                                                                    \
             PyErr_SetString(PyExc_RuntimeError, #name " is not bound");                     \
+            return NULL;                                                                    \
+        }                                                                                   \
+        look_at(0, __VA_ARGS__);                                                            \
+        if (wide) {                                                                         \
+            PyErr_SetString(PyExc_OverflowError, #name " takes sizes of 32 bits here");     \
             return NULL;                                                                    \
         }                                                                                   \
         Py_BEGIN_ALLOW_THREADS status = p_##name(__VA_ARGS__);                              \
