@@ -126,11 +126,16 @@ __device__ __forceinline__ void join_keys(K &one, K &two, int d) {
     two = max(min(one, other), max(two, second));
     one = max(one, other);
 }
-// (key 0 has no value; `low`: bits of a key that are not part of it)
+// (key 0 has no value; `low`: bits of a key that are not part of it.  In 32 bits a sum below the range counts as the lowest finite value: more
+// than that of a group with nothing left, and never apart from its like, which leaves their order to 64 bits.  Above the range it
+// is +inf, which is not apart from anything either.)
 template <typename K>
 __device__ __forceinline__ auto value_of(const RouteArgs &a, K one, K two, K low) {
     decltype(unordered(one)) none = -INFINITY, v = one ? unordered(one & ~low) : none;
-    if (a.group_best == 2) v += two ? unordered(two & ~low) : none;
+    if (a.group_best == 2) {
+        v = two ? v + unordered(two & ~low) : none;
+        if constexpr (sizeof(K) == 4) v = two ? fmaxf(v, -FLT_MAX) : v;
+    }
     return v;
 }
 
