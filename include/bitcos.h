@@ -662,8 +662,8 @@ int bitcos_fp8_quantize(const void *x, int x_type, int64_t rows, int64_t K, uint
  *   rows     0 .. BITCOS_FP8_ROWS_MAX (0: nothing is done); M and K as large, K a multiple of 128
  *   y        device [rows][M] of y_type (BITCOS_FP32 or BITCOS_BF16), 16-byte aligned, overwritten
  *   workspace   NULL, or device scratch of BITCOS_FP8_WORKSPACE_BYTES, zero filled once (bitcos_workspace_init), whose word 0 is
- *               the status word that bitcos_workspace_status reads (1: a bounded wait ran out, the outputs are not complete).  Nothing else is
- *               kept in it, so calls may share one.
+ *               the status word that bitcos_workspace_status reads (bit 0: a bounded wait ran out, the outputs are not complete; bit 1: see
+ *               bitcos_fp8_matmul_grouped; bits stay until the caller clears them).  Nothing else is kept in it, so calls may share one.
  * Stream ordered like the products: W (and nothing else) may be read while an earlier kernel of this library is still running, so
  * codes that bitcos_fp8_quantize has just written are activations, not weights, of the next call. */
 int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t K, const uint8_t *x, const float *x_scale, int64_t rows,
@@ -678,8 +678,8 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
  *   pair_xrow   device int32 [n_pairs], or NULL: pair p reads row p (the second product of an expert)
  *   x        device bytes [n_xrows][K];  x_scale   device float [n_xrows][K/128];  y   device [n_pairs][M]
  * The lists are checked on the device: a group whose expert is outside [0, n_experts) or whose pairs lie outside [0, n_pairs) is
- * skipped whole, a pair whose row is outside [0, n_xrows) alone; nothing of them is written and the status word is set
- * to 2.  An empty group is skipped without a mark.  Groups do not overlap (which of two writes a row that both cover is not said).
+ * skipped whole, a pair whose row is outside [0, n_xrows) alone; nothing of them is written and bit 1 of the status word is
+ * set (the word is then 2, or 3 where a wait has run out too).  An empty group (group_begin[i+1] <= group_begin[i]) is skipped without a mark.  Groups do not overlap (which of two writes a row that both cover is not said).
  * Rows of y that no group covers are left as they were.  W is read after every earlier kernel in the stream has completed.
  * Everything else as for bitcos_fp8_matmul. */
 int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_experts, int64_t M, int64_t K, const int32_t *group_expert,

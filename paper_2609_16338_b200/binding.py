@@ -1045,7 +1045,8 @@ class Fp8Weights:
 
 
 def make_fp8_workspace(device="cuda"):
-    """Zero-filled device scratch for the e4m3 products: their status word (workspace_status)."""
+    """Zero-filled device scratch for the e4m3 products: their status word (workspace_status: bit 0 a bounded wait ran out, bit 1 a
+    list was malformed; bits stay until the workspace is zeroed)."""
     import torch
     return torch.zeros(FP8_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 

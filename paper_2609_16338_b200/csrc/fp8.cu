@@ -135,6 +135,12 @@ struct Fp8Args {
     int max_groups, n_experts, n_xrows;
 };
 
+// The status word: a bit for each kind of trouble, so that none hides another (calls that run at the same time may share the word).
+constexpr unsigned int kGaveUp = 1, kBadList = 2;
+__device__ __forceinline__ void mark(const Fp8Args &a, unsigned int what) {
+    if (a.status) atomicOr(a.status, what);
+}
+
 struct Tile {
     int64_t row0;               // first token / pair
     int rows;                   // tokens / pairs of the tile
@@ -523,7 +529,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                         // a malformed group is skipped whole and marked (an empty one without a mark)
                         if (e >= 0 && e < a.n_experts && begin >= 0 && end <= a.rows)
                             tiles = static_cast<int64_t>((end - begin + L::kTileRows - 1) / L::kTileRows) * a.w_tiles;
-                        else if (a.status && blockIdx.x == 0) *a.status = 2u;
+                        else if (blockIdx.x == 0) mark(a, kBadList);
                     }
                 }
 #pragma unroll
@@ -541,7 +547,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         n_tiles = lists->tiles[n_groups];
         if (splits > 1 && n_tiles > t_step) {                // (a cluster adds up one tile; groups that do not overlap have no more)
             n_tiles = t_step;
-            if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = 2u;
+            if (blockIdx.x == 0 && threadIdx.x == 0) mark(a, kBadList);
         }
     }
     constexpr uint32_t kXBytes = PAIR ? kABytes : L::kBBytes;
@@ -745,7 +751,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 bool mine = row < tile.rows;
                 if (GROUPED && mine && (xr < 0 || xr >= a.n_xrows)) {
                     mine = false;
-                    if (a.status) *a.status = 2u;
+                    mark(a, kBadList);
                 }
                 const float *xs = row_scales();
                 ws = column_scales(tile);
@@ -907,7 +913,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     bad[j] = __ballot_sync(kFull, wrong);
                     if (wrong) {
                         there = false;
-                        if (a.status) *a.status = 2u;
+                        mark(a, kBadList);
                     }
                     xs[j] = there ? a.x_scale + xr * a.G : nullptr;
                     sx[j] = there ? __ldg(xs[j] + k0) : 0.f;
@@ -977,7 +983,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             }
         }
     }
-    if (!ok && a.status) *a.status = 1u;
+    if (!ok) mark(a, kGaveUp);
     if constexpr (PAIR) {                  // (the outputs are in memory before the block goes)
         if (warp >= L::kFirst && elect_one()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();

@@ -34,3 +34,24 @@ def test_group_sums_behind_the_range_of_32_bits(bc, experts, n_groups, score):
             for dtype in (torch.float32, torch.bfloat16):
                 check_route(bc, torch.from_numpy(z).cuda().to(dtype), bias, top_k=4, score=score, n_groups=n_groups, top_groups=top_groups,
                             group_best=2)
+
+
+@pytest.mark.parametrize("n_pairs,max_groups", [(40, 10), (200, 2)])
+def test_marks_in_the_status_word_do_not_replace_one_another(bc, n_pairs, max_groups):
+    """Calls may share the word: what one of them has said of a wait that ran out stays beside what another says of its lists."""
+    w, ws = weights(2, 256, 512, 1)
+    x, xs = activations(n_pairs, 512, 2)
+    ge, gb = (torch.zeros(max_groups + i, dtype=torch.int32, device="cuda") for i in (0, 1))
+    gb[1] = n_pairs
+    xr = torch.arange(n_pairs, dtype=torch.int32, device="cuda")
+    bad_row = xr.clone()
+    bad_row[3] = n_pairs
+    one, W = torch.ones(1, dtype=torch.int32, device="cuda"), bc.Fp8Weights(w, ws)
+    for lists in ((ge + 7, gb, xr), (ge, gb, bad_row)):
+        for before in (0, 1, 2, 3):
+            space = bc.make_fp8_workspace()
+            space[0] = before
+            bc.bitcos_fp8_matmul_grouped(W, lists[0], lists[1], one, lists[2], x, xs, workspace=space)
+            assert bc.workspace_status(space) == (before | 2)
+            bc.bitcos_fp8_matmul_grouped(W, ge, gb, one, xr, x, xs, workspace=space)
+            assert bc.workspace_status(space) == (before | 2)
