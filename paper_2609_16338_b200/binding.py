@@ -14,6 +14,7 @@ from dataclasses import dataclass
 import numpy as np
 
 GROUP = 128
+GROUP_EXPERTS_MAX = 1024            # BITCOS_GROUP_EXPERTS_MAX
 TILE_ROWS = 32
 MAX_BATCH = 16
 
@@ -973,12 +974,17 @@ def make_group_workspace(n_pairs: int, n_experts: int, device="cuda"):
 def bitcos_group_pairs_slots(expert, n_experts: int, workspace=None):
     """Groups the pairs of expert (int32 [tokens, top_k], as bitcos_route_experts returns it; any number of pairs) by expert:
     returns (group_expert, group_begin, pair_xrow_sorted, order, slot, n_groups), device int32 tensors; slot [tokens, top_k] is every
-    pair's place in the sorted lists, -1 for pairs left out."""
+    pair's place in the sorted lists, -1 for pairs left out.  Without tokens: empty lists and no groups."""
     import torch
     _require(expert.dtype == torch.int32 and expert.dim() == 2 and expert.is_contiguous(), "expert must be a contiguous int32 [tokens, top_k] tensor")
     tokens, top_k = expert.shape
     P = tokens * top_k
     stream = _stream_of(expert, workspace)
+    if tokens == 0:
+        # (the C function takes one pair or more)
+        _require(top_k > 0 and 1 <= n_experts <= GROUP_EXPERTS_MAX, f"expert must have places and n_experts be 1 to {GROUP_EXPERTS_MAX}")
+        none, zero = expert.new_empty(0), expert.new_zeros(2)
+        return none, zero[:1], none.clone(), none.clone(), torch.empty_like(expert), zero[1:]
     if workspace is None:
         workspace = make_group_workspace(P, n_experts, expert.device)
     cap = min(P, n_experts)
@@ -996,7 +1002,7 @@ def bitcos_group_pairs_slots(expert, n_experts: int, workspace=None):
 
 def bitcos_combine_pairs(y, slot, weight, base=None, out=None, out_dtype=None):
     """out[t] = base[t] + sum over j of weight[t, j] * y[slot[t, j]]: y [rows, M] (float32 or bfloat16), slot int32 and weight
-    float32 [tokens, top_k] (a slot outside the rows adds nothing), base and out [tokens, M] of one type (float32 or bfloat16;
+    float32 [tokens, top_k] (a slot outside the rows adds nothing; y may have no rows), base and out [tokens, M] of one type (float32 or bfloat16;
     out_dtype, else base's, else y's).  base may be out."""
     import torch
     _require(y.dim() == 2 and y.is_contiguous(), "y must be a contiguous [rows, M] tensor")
@@ -1010,6 +1016,9 @@ def bitcos_combine_pairs(y, slot, weight, base=None, out=None, out_dtype=None):
     _require(base is None or (base.shape == out.shape and base.dtype == out.dtype and base.is_contiguous()), "base must be shaped and typed as out")
     y_code, out_code = _type_code(y.dtype, (0, 1), "y"), _type_code(out.dtype, (0, 1), "out")
     stream = _stream_of(y, slot, weight, base, out)
+    if rows == 0 and top_k > 0 and M > 0:
+        # (no slot names a row; the C function takes one row or more)
+        return out.zero_() if base is None else out.copy_(base)
     status = (_calls or _native()).bitcos_combine_pairs(
         y.data_ptr(), y_code, rows, slot.data_ptr(), weight.data_ptr(), tokens, top_k, M, 0 if base is None else base.data_ptr(),
         out.data_ptr(), out_code, stream) if tokens else 0

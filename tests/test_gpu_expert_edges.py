@@ -55,3 +55,52 @@ def test_marks_in_the_status_word_do_not_replace_one_another(bc, n_pairs, max_gr
             assert bc.workspace_status(space) == (before | 2)
             bc.bitcos_fp8_matmul_grouped(W, ge, gb, one, xr, x, xs, workspace=space)
             assert bc.workspace_status(space) == (before | 2)
+
+
+def test_a_layer_without_tokens(bc):
+    """Every call of a routed layer takes a batch of no tokens, recorded in a graph too; a sum whose y has no rows is its base, or zero."""
+    E, k, H, M = 12, 4, 256, 384
+    w, ws = weights(E, M, H, 1)
+    W, space = bc.Fp8Weights(w, ws), bc.make_fp8_workspace()
+
+    def layer(x, logits):
+        expert, weight, _ = bc.bitcos_route_experts(logits, k)
+        ge, gb, xr, order, slot, ng = bc.bitcos_group_pairs_slots(expert, E)
+        q, s = bc.bitcos_fp8_quantize(x)
+        y = bc.bitcos_fp8_matmul_grouped(W, ge, gb, ng, xr, q, s, workspace=space)
+        return ge, gb, xr, order, slot, ng, y, bc.bitcos_combine_pairs(y, slot, weight)
+
+    def check_empty(ge, gb, xr, order, slot, ng, y, out):
+        assert all(t.dtype == torch.int32 and t.is_cuda for t in (ge, gb, xr, order, slot, ng))
+        assert (ge.shape, gb.tolist(), xr.shape, order.shape, slot.shape, ng.tolist()) == ((0,), [0], (0,), (0,), (0, k), [0])
+        assert y.shape == (0, M) and out.shape == (0, M)
+
+    x, logits = torch.empty(0, H, device="cuda"), torch.empty(0, E, device="cuda")
+    check_empty(*layer(x, logits))
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        out = layer(x, logits)
+    graph.replay()
+    torch.cuda.synchronize()
+    check_empty(*out)
+    for dtype in (torch.float32, torch.bfloat16):
+        y = torch.empty(0, M, dtype=dtype, device="cuda")
+        slot, weight = torch.zeros(5, k, dtype=torch.int32, device="cuda"), torch.full((5, k), float("nan"), device="cuda")
+        base = torch.randn(5, M, device="cuda")
+        assert (bc.bitcos_combine_pairs(y, slot, weight, out_dtype=torch.float32) == 0).all()
+        got = bc.bitcos_combine_pairs(y, slot, weight, base=base)
+        assert torch.equal(got, base) and got.data_ptr() != base.data_ptr()
+        kept = base.clone()
+        assert bc.bitcos_combine_pairs(y, slot, weight, base=base, out=base) is base and torch.equal(base, kept)
+    # what is refused with tokens is refused without
+    empty = torch.empty(0, k, dtype=torch.int32, device="cuda")
+    for bad in (0, 1025, -1):
+        with pytest.raises((ValueError, bc.BitcosError)):
+            bc.bitcos_group_pairs_slots(empty, bad)
+    with pytest.raises((ValueError, bc.BitcosError)):
+        bc.bitcos_group_pairs_slots(torch.empty(0, 0, dtype=torch.int32, device="cuda"), E)
+    with pytest.raises(ValueError):
+        bc.bitcos_group_pairs_slots(empty.cpu(), E)
+    with pytest.raises(ValueError):
+        bc.bitcos_combine_pairs(y, slot, weight, out=torch.empty(5, M, dtype=torch.float16, device="cuda"))
