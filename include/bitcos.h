@@ -687,6 +687,16 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
                               int64_t n_pairs, const uint8_t *x, const float *x_scale, int64_t n_xrows, void *y, int y_type, void *workspace,
                               size_t workspace_bytes, void *cuda_stream);
 
+/* Both with the limit of the waits that a kernel's warps have for one another given: nanoseconds (half a second otherwise), or,
+ * below 1000, how often a wait looks again before it gives up.  Where one runs out the block stops, what is under way is waited for, and
+ * bit 0 of the status word is set: the outputs are not complete, the device stays usable, and the next call is an ordinary one. */
+int bitcos_fp8_matmul_limited(const uint8_t *W, const float *w_scale, int64_t M, int64_t K, const uint8_t *x, const float *x_scale, int64_t rows,
+                              void *y, int y_type, void *workspace, size_t workspace_bytes, uint64_t wait_limit_ns, void *cuda_stream);
+int bitcos_fp8_matmul_grouped_limited(const uint8_t *W, const float *w_scale, int n_experts, int64_t M, int64_t K, const int32_t *group_expert,
+                                      const int32_t *group_begin, const int32_t *n_groups_device, int max_groups, const int32_t *pair_xrow,
+                                      int64_t n_pairs, const uint8_t *x, const float *x_scale, int64_t n_xrows, void *y, int y_type, void *workspace,
+                                      size_t workspace_bytes, uint64_t wait_limit_ns, void *cuda_stream);
+
 #ifdef __GNUC__
 #pragma GCC visibility pop
 #endif

@@ -31,7 +31,7 @@ EXPORTED_SYMBOLS = [
     "bitcos_choose_format", "bitcos_count_nnz_device", "bitcos_pack_device", "bitcos_pack_device_limited", "bitcos_gemv_bf16", "bitcos_gemv_multi_bf16",
     "bitcos_gemv_multi_group_scales", "bitcos_gemv_blend_bf16", "bitcos_decode_probe_variant", "bitcos_gemv_phased", "bitcos_gemv_phases_host", "trit5_gemv_grouped", "bit2_gemv_grouped", "bitcos_gemv_static_status", "bitcos_wait_probe", "bitcos_group_pairs_device", "bitcos_gemv_grouped_lists", "bitcos_gemv_multi_chained", "bitcos_gemv_multi_plan",
     "bitcos_route_experts", "bitcos_group_workspace_bytes", "bitcos_group_pairs_slots", "bitcos_combine_pairs",
-    "bitcos_fp8_quantize", "bitcos_fp8_matmul", "bitcos_fp8_matmul_grouped",
+    "bitcos_fp8_quantize", "bitcos_fp8_matmul", "bitcos_fp8_matmul_grouped", "bitcos_fp8_matmul_limited", "bitcos_fp8_matmul_grouped_limited",
 ]
 
 
@@ -138,6 +138,8 @@ def load_library():
     L.bitcos_fp8_quantize.argtypes = [vp, C.c_int, i64, i64, vp, vp, vp]
     L.bitcos_fp8_matmul.argtypes = [vp, vp, i64, i64, vp, vp, i64, vp, C.c_int, vp, sz, vp]
     L.bitcos_fp8_matmul_grouped.argtypes = [vp, vp, C.c_int, i64, i64, vp, vp, vp, C.c_int, vp, i64, vp, vp, i64, vp, C.c_int, vp, sz, vp]
+    L.bitcos_fp8_matmul_limited.argtypes = [*L.bitcos_fp8_matmul.argtypes[:-1], u64, vp]
+    L.bitcos_fp8_matmul_grouped_limited.argtypes = [*L.bitcos_fp8_matmul_grouped.argtypes[:-1], u64, vp]
     _bind_calls(L)
     _lib = L
     return L

@@ -116,12 +116,21 @@ constexpr int kMaxSplits = 8;             // portable cluster size
 // front and the promoters split it into.
 constexpr int kLaunchRegisters = 168, kFrontRegisters = 72, kPromoterRegisters = 216;
 
+// How long a wait goes on, and for how long at a time it sleeps.
+struct Patience {
+    uint64_t limit_ns;
+    uint32_t sleep_ns;
+};
+constexpr uint32_t kSleepNs = 1000000;
+constexpr uint64_t kLooks = 1000;         // a limit below this is a number of looks
+
 struct Fp8Args {
     const float *w_scale;       // [experts][w_blocks][G]
     const float *x_scale;       // [x rows][G]
     const uint8_t *x;           // grouped: rows to gather
     void *y;
     unsigned int *status;       // NULL, or the workspace's status word
+    Patience patience;          // of the waits that the roles have for one another
     int64_t M;
     int64_t rows;               // dense: tokens; grouped: pairs
     int G;                      // groups of 128 along K
@@ -198,7 +207,8 @@ struct Layout {
     static constexpr uint32_t kTiles = kBars + (3 * kStages + 2 * kAcc + 1 + kTileRing) * 8;
     static constexpr uint32_t kRows = kTiles + kTileRing * sizeof(Tile);
     static constexpr uint32_t kTmem = kRows + (GROUPED ? 2 * kRowsPerTile * 4 : 0);
-    static constexpr uint32_t kScales = (kTmem + 4 + 15) / 16 * 16;
+    static constexpr uint32_t kEnds = (kTmem + 4 + 15) / 16 * 16;       // PAIR: how far both blocks got
+    static constexpr uint32_t kScales = kEnds + (PAIR ? 32 : 0);
     static constexpr uint32_t kPrefix = kScales + (PAIR ? 0 : kPromoters * 2 * N * 4);
     static constexpr uint32_t kTotal = kPrefix + (GROUPED ? sizeof(GroupLists) : 0);
     static constexpr uint32_t kDynamic = kTotal + 1024;  // (the stages start on a 1024-byte boundary)
@@ -314,14 +324,14 @@ __device__ __forceinline__ bool elect_one() {
 }
 // Asks whether a phase is complete, asleep for up to a millisecond until it is.  (Without the time a question returns at once, and ten
 // warps that keep asking leave every other access to shared memory 600 clocks in the queue.)
-__device__ __forceinline__ uint32_t ask(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ uint32_t ask(uint32_t bar, uint32_t parity, uint32_t sleep_ns) {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
-        : "r"(bar), "r"(parity), "r"(1000000u)
+        : "r"(bar), "r"(parity), "r"(sleep_ns)
         : "memory");
     return done;
 }
@@ -338,17 +348,32 @@ __device__ __forceinline__ uint32_t test(uint32_t bar, uint32_t parity) {
     return done;
 }
 // A bounded wait.  (No call in it: with one, ptxas keeps every role to the registers that the block is launched with.)
-__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity, const Patience &p) {
     uint64_t t0 = 0;
-    while (!ask(bar, parity)) {
+    while (!ask(bar, parity, p.sleep_ns)) {
         const uint64_t now = global_timer_ns();
         if (t0 == 0) t0 = now;
-        else if (now - t0 > kWaitLimitNs) return false;
+        if (now - t0 >= p.limit_ns) return false;
     }
     return true;
 }
-// A bounded wait by a whole warp, which goes on or gives up as one (what follows are instructions of whole warps).
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(kFull, wait_here(bar, parity)); }
+// The same with so little patience that a number of looks decides: a question sleeps for a while whatever time it is given.
+__device__ __forceinline__ bool look_here(uint32_t bar, uint32_t parity, const Patience &p) {
+    for (uint32_t i = 0; i <= p.sleep_ns; ++i)
+        if (test(bar, parity)) return true;
+    return false;
+}
+// A bounded wait by a whole warp, which goes on or gives up as one (what follows are instructions of whole warps).  PATIENT is one of the
+// kernel's parameters because the choice at run time, in every wait, cost 1.5 %.
+template <bool PATIENT>
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const Patience &p) {
+    return __all_sync(kFull, PATIENT ? wait_here(bar, parity, p) : look_here(bar, parity, p));
+}
+// The same for what is under way already and arrives by itself, whatever the roles have given up.
+__device__ __forceinline__ bool drain_wait(uint32_t bar, uint32_t parity) {
+    constexpr Patience p{kWaitLimitNs, kSleepNs};
+    return warp_wait<true>(bar, parity, p);
+}
 // a += d * s, two at a time
 __device__ __forceinline__ void fma_pair(float &a0, float &a1, uint32_t d0, uint32_t d1, float s0, float s1) {
     asm("{\n\t.reg .b64 a, d, s;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 d, {%2, %3};\n\tmov.b64 s, {%4, %5};\n\t"
@@ -383,6 +408,13 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank
 // barrier has seen land in this block's shared memory, where this multiprocessor's own tensor cores read them.)
 __device__ __forceinline__ void cluster_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_store(uint32_t addr, uint32_t rank, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_address(addr, rank)), "r"(v) : "memory");
+}
+// Takes bytes that will not come off a phase.
+__device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
@@ -426,7 +458,7 @@ __device__ __forceinline__ Tile find_tile(const Fp8Args &a, const GroupLists *li
     return r;
 }
 
-template <int N, bool PAIR, bool GROUPED>
+template <int N, bool PAIR, bool GROUPED, bool PATIENT>
 __global__ void __launch_bounds__(Layout<N, PAIR, GROUPED>::kThreads, Layout<N, PAIR, GROUPED>::kBlocks)
 fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap,
                   const __grid_constant__ Fp8Args a) {
@@ -456,6 +488,12 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         if constexpr (PAIR) tma_3d_pair(dst, &wmap, kb * kGroup, t.w0 + rank * L::kBRows, t.expert, bar);
         else tma_3d(dst, &wmap, kb * kGroup, t.w0, t.expert, bar);
     };
+    // PAIR: how far the two blocks got, words that both have: stages sent by each, stages of routed rows that the second has
+    // announced, stages multiplied, whether any wait has run out
+    constexpr int kIssued = 0, kAnnounced = 2, kMultiplied = 3, kStopped = 4;
+    const auto tell = [&](int word, uint32_t v) {
+        for (uint32_t r = 0; r < 2; ++r) cluster_store(base + L::kEnds + 4 * word, r, v);
+    };
     // the first weights are on their way before the kernel in front of this one has finished: they are nobody's output
     const auto send_first = [&]() {
         if (t_first < static_cast<int64_t>(a.row_tiles) * a.w_tiles) {
@@ -479,6 +517,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
         mbar_init(drained, 1);
         for (int i = 0; i < kTileRing; ++i) mbar_init(told + 8 * i, 1);
+        if (PAIR) *reinterpret_cast<volatile uint32_t *>(smem + L::kEnds + 4 * kStopped) = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         if (!GROUPED && !PAIR) send_first();
     }
@@ -555,7 +594,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     uint32_t it = 0;                       // groups of 128 so far, over all tiles
     uint32_t tiles = 0;                    // tiles so far
     const auto next_tile = [&](Tile &t) {  // the block's next tile, from the ring
-        if (!warp_wait(told + 8 * (tiles % kTileRing), (tiles / kTileRing) & 1)) return false;
+        if (!warp_wait<PATIENT>(told + 8 * (tiles % kTileRing), (tiles / kTileRing) & 1, a.patience)) return false;
         t = ring[tiles++ % kTileRing];
         return true;
     };
@@ -579,7 +618,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 for (int kb = k0; ok && kb < k1; ++kb, ++it) {
                     const uint32_t s = at.s;
                     const uint32_t x_dst = base + s * L::kStageBytes + (PAIR ? 0 : kABytes);
-                    if (it >= kStages && !warp_wait(empty + 8 * s, at.phase ^ 1)) {
+                    if (it >= kStages && !warp_wait<PATIENT>(empty + 8 * s, at.phase ^ 1, a.patience)) {
                         ok = false;
                         break;
                     }
@@ -598,9 +637,14 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     at.next();
                 }
             }
-            // no copy may outlive the block, and (PAIR) no arrival from the other block's products: every stage has been read
-            for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
-                ok = warp_wait((PAIR ? empty : full) + 8 * (i % kStages), (i / kStages) & 1);
+            // no copy may outlive the block, also where a wait has run out; PAIR: nor an arrival from the other block's products,
+            // so every stage has been read (if not, both blocks settle what is left, below)
+            for (uint32_t i = it > kStages ? it - kStages : 0; (ok || !PAIR) && i < it; ++i) {
+                if (PAIR) ok = warp_wait<PATIENT>(empty + 8 * (i % kStages), (i / kStages) & 1, a.patience);
+                else ok &= drain_wait(full + 8 * (i % kStages), (i / kStages) & 1);
+            }
+            if (PAIR && elect_one()) tell(kIssued + rank, it);
+            __syncwarp();
         } else if (warp == 1) {
             // ---- tensor cores: the warp waits, one lane issues
             constexpr uint32_t idesc = instruction_desc(PAIR ? 2 * kARows : kARows, N);
@@ -612,12 +656,13 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     const uint32_t s = at.s, b = it % L::kAcc, again = (it / L::kAcc & 1) ^ 1;
                     // (the barriers are asked before any answer is looked at: an answer takes about 200 clocks here, and
                     // this warp's turn has to stay below the 512 clocks of its products)
-                    const uint32_t have = ask(full + 8 * s, at.phase);
-                    const uint32_t rows = !gather || ask(gathered + 8 * s, at.phase);
-                    const uint32_t room = it < L::kAcc || ask(acc_empty + 8 * b, again);
+                    const auto there = [&](uint32_t bar, uint32_t parity) { return PATIENT ? ask(bar, parity, a.patience.sleep_ns) : test(bar, parity); };
+                    const uint32_t have = there(full + 8 * s, at.phase);
+                    const uint32_t rows = !gather || there(gathered + 8 * s, at.phase);
+                    const uint32_t room = it < L::kAcc || there(acc_empty + 8 * b, again);
                     if (!__all_sync(kFull, have & room & rows)) {
-                        if ((it >= L::kAcc && !warp_wait(acc_empty + 8 * b, again)) || !warp_wait(full + 8 * s, at.phase) ||
-                            (gather && !warp_wait(gathered + 8 * s, at.phase))) {
+                        if ((it >= L::kAcc && !warp_wait<PATIENT>(acc_empty + 8 * b, again, a.patience)) || !warp_wait<PATIENT>(full + 8 * s, at.phase, a.patience) ||
+                            (gather && !warp_wait<PATIENT>(gathered + 8 * s, at.phase, a.patience))) {
                             ok = false;
                             break;
                         }
@@ -641,7 +686,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             for (int64_t t = t_first; gather && !issues && ok && t < n_tiles; t += t_step) {
                 for (int kb = k0; kb < k1; ++kb, ++it) {
                     const uint32_t s = it % kStages;
-                    if (!warp_wait(gathered + 8 * s, (it / kStages) & 1)) {
+                    if (!warp_wait<PATIENT>(gathered + 8 * s, (it / kStages) & 1, a.patience)) {
                         ok = false;
                         break;
                     }
@@ -654,8 +699,10 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             if (issues) {
                 if (elect_one()) mma_commit<PAIR, true>(drained);
                 __syncwarp();
-                ok &= warp_wait(drained, 0);
+                ok &= drain_wait(drained, 0);
             }
+            if (PAIR && elect_one()) tell(issues ? kMultiplied : kAnnounced, it);
+            __syncwarp();
         } else if (L::kFirst == 4 && warp < L::kFirst) {
             // ---- rows of routed pairs: two warps take the stages in turn; eight lanes per row of 128 bytes, 16 bytes each, put where the
             // 128-byte swizzle has them.  Bound by the copies: 512 bytes take an instruction of these about 18 clocks.
@@ -684,7 +731,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     __syncwarp();
                     for (int kb = k0; kb < k1; ++kb, ++it, at.next()) {
                         if ((it & 1) != turn) continue;
-                        if (it >= kStages && !warp_wait(empty + 8 * at.s, at.phase ^ 1)) {
+                        if (it >= kStages && !warp_wait<PATIENT>(empty + 8 * at.s, at.phase ^ 1, a.patience)) {
                             ok = false;
                             break;
                         }
@@ -706,6 +753,9 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     }
                 }
                 asm volatile("cp.async.wait_all;" ::: "memory");
+                // (their arrivals too: the last rounds of this warp)
+                for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
+                    if ((i & 1) == turn) ok &= drain_wait(gathered + 8 * (i % kStages), (i / kStages) & 1);
             }
         }
     } else {
@@ -760,7 +810,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                 float scale = sx0 * sw0, sx = sx1, sw = sw1;
                 const bool more = t + t_step < n_tiles;
                 uint32_t d[2][32];
-                ok = warp_wait(acc_full + 8 * (it % L::kAcc), (it / L::kAcc) & 1);
+                ok = warp_wait<PATIENT>(acc_full + 8 * (it % L::kAcc), (it / L::kAcc) & 1, a.patience);
                 if (ok) {
                     tmem_fence_after();
                     tmem_load32(tmem_row + (it % L::kAcc) * N, d[0]);
@@ -798,7 +848,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                             for (int i = 0; i < 32; i += 2) fma_pair(acc[c * 32 + i], acc[c * 32 + i + 1], d[c & 1][i], d[c & 1][i + 1], s, s);
                         }
                         if (kb + 1 < k1) {
-                            ok = __all_sync(kFull, next) || warp_wait(acc_full + 8 * (it % L::kAcc), (it / L::kAcc) & 1);
+                            ok = __all_sync(kFull, next) || warp_wait<PATIENT>(acc_full + 8 * (it % L::kAcc), (it / L::kAcc) & 1, a.patience);
                             if (ok) {
                                 tmem_fence_after();
                                 tmem_load32(tmem_row + (it % L::kAcc) * N, d[0]);
@@ -808,7 +858,10 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     if (more && ok && run == 0) look_up();
                     if (more && ok && run == 1) first_scales();
                 }
-                if (!ok) break;
+                if (!ok) {
+                    tmem_wait32(d[0]);                   // (may be on its way: the look ahead may have given up)
+                    break;
+                }
                 const int64_t c0 = tile.w0 + part * kCols;
                 // A thread has a row, memory wants lines: each warp puts its 32 rows into shared memory, two boxes of 128 bytes of a row at
                 // a time, and TMA writes them while the next tile's groups are added.  (Stored by the warp itself, line by line, a tile
@@ -932,7 +985,7 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
                     sw = sw_next;
                     if (kb + 2 < k1) sw_next = __ldg(ws + kb + 2);
                     __syncwarp();
-                    if (!warp_wait(acc_full + 8 * b, (it / L::kAcc) & 1)) {
+                    if (!warp_wait<PATIENT>(acc_full + 8 * b, (it / L::kAcc) & 1, a.patience)) {
                         ok = false;
                         break;
                     }
@@ -983,7 +1036,10 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
             }
         }
     }
-    if (!ok) mark(a, kGaveUp);
+    if (!ok) {
+        mark(a, kGaveUp);
+        if (PAIR) tell(kStopped, 1);
+    }
     if constexpr (PAIR) {                  // (the outputs are in memory before the block goes)
         if (warp >= L::kFirst && elect_one()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
@@ -1028,8 +1084,36 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
         }
     }
     tmem_fence_before();
-    if constexpr (PAIR) cluster_sync();                      // (neither block goes while the other's copies or products may reach it)
-    else __syncthreads();
+    if constexpr (PAIR) {
+        cluster_sync();                    // (neither block goes while the other's copies or products may reach it)
+        const volatile uint32_t *ends = reinterpret_cast<const volatile uint32_t *>(smem + L::kEnds);
+        if (ends[kStopped]) {
+            // A wait has run out somewhere, and the blocks stopped at different stages (no two more than the ring apart: a stage
+            // is filled again only when its products are done).  The first block makes up for the arrivals and bytes that will not come, so
+            // that the phases complete when the copies of both blocks that are under way have landed; both blocks wait for the
+            // arrivals that stand for products.
+            if (warp == 0) {
+                const uint32_t sent0 = ends[kIssued], sent1 = ends[kIssued + 1], rows1 = ends[kAnnounced], products = ends[kMultiplied];
+                const uint32_t bytes = gather ? L::kStageBytes - kXBytes : L::kStageBytes;
+                const uint32_t top = max(max(sent0, sent1), gather ? rows1 : 0u);
+                for (uint32_t i = top > kStages ? top - kStages : 0; rank == 0 && i < top; ++i) {
+                    const uint32_t bar = full + 8 * (i % kStages);
+                    if (elect_one()) {
+                        if (i >= sent0 && i < sent1) mbar_expect_tx(bar, bytes);
+                        else if (i >= sent0) mbar_arrive(bar);
+                        else if (i >= sent1) mbar_complete_tx(bar, bytes);
+                        if (gather && i >= rows1) mbar_arrive(bar);
+                    }
+                    __syncwarp();
+                    drain_wait(bar, (i / kStages) & 1);
+                }
+                for (uint32_t i = products > kStages ? products - kStages : 0; i < products; ++i) drain_wait(empty + 8 * (i % kStages), (i / kStages) & 1);
+                for (uint32_t i = products > L::kAcc ? products - L::kAcc : 0; i < products; ++i) drain_wait(acc_full + 8 * (i % L::kAcc), (i / L::kAcc) & 1);
+            }
+            __syncwarp();
+            cluster_sync();
+        }
+    } else __syncthreads();
     if (warp == 1) {
         tmem_fence_after();
         if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kTmemColumns) : "memory");
@@ -1092,10 +1176,10 @@ int encode_outputs(CUtensorMap *map, const Fp8Args &a) {
 }
 
 // Once per kernel and device, as in prepare_kernel, and all of the cache as shared memory.
-template <int N, bool PAIR, bool GROUPED>
+template <int N, bool PAIR, bool GROUPED, bool PATIENT>
 int prepare_fp8(int dev) {
     using L = Layout<N, PAIR, GROUPED>;
-    auto *kernel = fp8_matmul_kernel<N, PAIR, GROUPED>;
+    auto *kernel = fp8_matmul_kernel<N, PAIR, GROUPED, PATIENT>;
     static bool prepared[32];
     if (dev < 32 && prepared[dev]) return BITCOS_OK;
     int rc = BITCOS_OK;
@@ -1115,8 +1199,9 @@ int prepare_fp8(int dev) {
     return rc;
 }
 
-template <int N, bool PAIR, bool GROUPED>
+template <int N, bool PAIR, bool GROUPED, bool PATIENT = true>
 int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_rows, const Fp8Args &args, int64_t blocks, cudaStream_t stream) {
+    if (PATIENT && args.patience.limit_ns < kLooks) return launch_fp8<N, PAIR, GROUPED, false>(W, x, K, experts, x_rows, args, blocks, stream);
     using L = Layout<N, PAIR, GROUPED>;
     static_assert(L::kStages + L::kAcc + 1 < kTileRing, "the producer's lead");
     static_assert(L::kBlocks * (L::kDynamic + 1024) <= 228 * 1024 && L::kBlocks * L::kTmemColumns <= 512, "the blocks of a multiprocessor");
@@ -1128,10 +1213,10 @@ int launch_fp8(const void *W, const void *x, int64_t K, int experts, int64_t x_r
     if (rc) return rc;
     if (PAIR && args.vector) rc = encode_outputs(&ymap, args);
     if (rc) return rc;
-    auto *kernel = fp8_matmul_kernel<N, PAIR, GROUPED>;
+    auto *kernel = fp8_matmul_kernel<N, PAIR, GROUPED, PATIENT>;
     int dev = 0;
     rc = check_cuda(cudaGetDevice(&dev));
-    if (rc == BITCOS_OK) rc = prepare_fp8<N, PAIR, GROUPED>(dev);
+    if (rc == BITCOS_OK) rc = prepare_fp8<N, PAIR, GROUPED, PATIENT>(dev);
     if (rc) return rc;
     static const char *env = std::getenv("BITCOS_PDL");
     cudaLaunchConfig_t cfg{};
@@ -1179,7 +1264,7 @@ int plan_weights_first(const Fp8Args &a, int64_t tiles, int sms, int *splits_out
     int dev = 0;
     int rc = check_cuda(cudaGetDevice(&dev));
     if (rc) return rc;
-    rc = prepare_fp8<N, false, GROUPED>(dev);
+    rc = prepare_fp8<N, false, GROUPED, true>(dev);
     if (rc) return rc;
     constexpr int64_t group_ns = N == 16 ? kGroupNs16 : N == 32 ? kGroupNs32 : kGroupNs64;
     *ns_out = INT64_MAX;
@@ -1196,7 +1281,7 @@ int plan_weights_first(const Fp8Args &a, int64_t tiles, int sms, int *splits_out
             attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
             cfg.attrs = &attr;
             cfg.numAttrs = 1;
-            rc = check_cuda(cudaOccupancyMaxActiveClusters(&clusters, fp8_matmul_kernel<N, false, GROUPED>, &cfg));
+            rc = check_cuda(cudaOccupancyMaxActiveClusters(&clusters, fp8_matmul_kernel<N, false, GROUPED, true>, &cfg));
             if (rc) return rc;
             clusters = Layout<N, false, GROUPED>::kBlocks * std::max(clusters, 1);      // (it counts one block per multiprocessor, whatever its size)
             if (dev < 32) held[dev][splits] = clusters;
@@ -1223,6 +1308,8 @@ int launch_weights_first(const void *W, const void *x, int64_t K, Fp8Args &a, in
     a.w_tiles = a.w_blocks;
     return launch_fp8<N, false, false>(W, x, K, 1, a.rows, a, row_tiles * a.w_blocks * a.splits, stream);
 }
+
+Patience patience_of(uint64_t limit_ns) { return Patience{limit_ns, static_cast<uint32_t>(std::min<uint64_t>(limit_ns, kSleepNs))}; }
 
 int status_word(void *workspace, size_t workspace_bytes, unsigned int **status) {
     *status = static_cast<unsigned int *>(workspace);
@@ -1251,6 +1338,11 @@ int bitcos_fp8_quantize(const void *x, int x_type, int64_t rows, int64_t K, uint
 
 int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t K, const uint8_t *x, const float *x_scale, int64_t rows,
                       void *y, int y_type, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    return bitcos_fp8_matmul_limited(W, w_scale, M, K, x, x_scale, rows, y, y_type, workspace, workspace_bytes, kWaitLimitNs, cuda_stream);
+}
+
+int bitcos_fp8_matmul_limited(const uint8_t *W, const float *w_scale, int64_t M, int64_t K, const uint8_t *x, const float *x_scale, int64_t rows,
+                              void *y, int y_type, void *workspace, size_t workspace_bytes, uint64_t wait_limit_ns, void *cuda_stream) {
     if (!W || !w_scale || !x || !x_scale || !y) return BITCOS_ERR_NULL;
     if (M < 1 || M > BITCOS_FP8_ROWS_MAX || K < kGroup || K % kGroup != 0 || K > BITCOS_FP8_ROWS_MAX || rows < 0 || rows > BITCOS_FP8_ROWS_MAX ||
         (y_type != BITCOS_FP32 && y_type != BITCOS_BF16))
@@ -1261,6 +1353,7 @@ int bitcos_fp8_matmul(const uint8_t *W, const float *w_scale, int64_t M, int64_t
     int rc = status_word(workspace, workspace_bytes, &a.status);
     if (rc) return rc;
     if (rows == 0) return BITCOS_OK;
+    a.patience = patience_of(wait_limit_ns);
     a.w_scale = w_scale;
     a.x_scale = x_scale;
     a.y = y;
@@ -1302,6 +1395,14 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
                               const int32_t *group_begin, const int32_t *n_groups_device, int max_groups, const int32_t *pair_xrow,
                               int64_t n_pairs, const uint8_t *x, const float *x_scale, int64_t n_xrows, void *y, int y_type, void *workspace,
                               size_t workspace_bytes, void *cuda_stream) {
+    return bitcos_fp8_matmul_grouped_limited(W, w_scale, n_experts, M, K, group_expert, group_begin, n_groups_device, max_groups, pair_xrow, n_pairs,
+                                             x, x_scale, n_xrows, y, y_type, workspace, workspace_bytes, kWaitLimitNs, cuda_stream);
+}
+
+int bitcos_fp8_matmul_grouped_limited(const uint8_t *W, const float *w_scale, int n_experts, int64_t M, int64_t K, const int32_t *group_expert,
+                                      const int32_t *group_begin, const int32_t *n_groups_device, int max_groups, const int32_t *pair_xrow,
+                                      int64_t n_pairs, const uint8_t *x, const float *x_scale, int64_t n_xrows, void *y, int y_type, void *workspace,
+                                      size_t workspace_bytes, uint64_t wait_limit_ns, void *cuda_stream) {
     if (!W || !w_scale || !group_expert || !group_begin || !n_groups_device || !x || !x_scale || !y) return BITCOS_ERR_NULL;
     if (M < 1 || M > BITCOS_FP8_ROWS_MAX || K < kGroup || K % kGroup != 0 || K > BITCOS_FP8_ROWS_MAX || n_experts < 1 || max_groups < 1 ||
         max_groups > kMaxGroups || n_pairs < 0 || n_pairs > BITCOS_FP8_ROWS_MAX || n_xrows < 1 || n_xrows > BITCOS_FP8_ROWS_MAX ||
@@ -1315,6 +1416,7 @@ int bitcos_fp8_matmul_grouped(const uint8_t *W, const float *w_scale, int n_expe
     int rc = status_word(workspace, workspace_bytes, &a.status);
     if (rc) return rc;
     if (n_pairs == 0) return BITCOS_OK;
+    a.patience = patience_of(wait_limit_ns);
     a.w_scale = w_scale;
     a.x_scale = x_scale;
     a.y = y;
