@@ -620,6 +620,8 @@ int bitcos_route_experts(const void *logits, int logits_type, int64_t row_stride
  * n_pairs / top_k tokens in order (pair i belongs to token i / top_k, which is what pair_xrow_sorted receives), and
  *   slot   device int32 [n_pairs]: where pair i stands in the sorted lists (-1: left out, its expert is out of range) --
  *          the row of the grouped products' outputs that bitcos_combine_pairs adds for it.
+ * For whatever bitcos_combine_pairs adds up afterwards, and for more than BITCOS_GROUP_PAIRS_MAX pairs; bitcos_group_pairs_device is for
+ * short lists whose rows are not the tokens in order (it takes pair_xrow), and gives no places.
  * The other lists as for bitcos_group_pairs_device, what the groups leave of them too: group_expert [min(n_pairs, n_experts)],
  * group_begin [min(n_pairs, n_experts) + 1], pair_xrow_sorted, order [n_pairs], n_groups [1].  n_pairs 1 .. 2^31 - 1.
  *   workspace   device scratch of bitcos_group_workspace_bytes(n_pairs, n_experts) bytes, contents of no matter before and
@@ -640,9 +642,10 @@ int bitcos_combine_pairs(const void *y, int y_type, int64_t n_rows, const int32_
                          int64_t M, const void *base, void *out, int out_type, void *cuda_stream);
 
 /* ---------------------------------------------------------------------------------------
- * 8-bit floating point (e4m3) beside the ternary formats: for the matrices that a ternary checkpoint keeps in
- * 8 bits, for prompts (any number of rows), and as the same-chip baseline at 8 bits per weight.  (The paper has no
- * counterpart; its 16-bit group scales along K are here 32-bit scales of blocks of 128 x 128.)
+ * 8-bit floating point (e4m3) beside the ternary formats: the same-chip baseline at 8 bits per weight, and for matrices
+ * kept in 8 bits, with any number of rows.  (The paper has no counterpart; its 16-bit group scales along K are here 32-bit
+ * scales of blocks of 128 x 128.)  The caller brings a weight's codes and scales: nothing here makes them, and the packed ternary
+ * formats, whose scales are per row and group, do not lead to them.
  * ------------------------------------------------------------------------------------- */
 #define BITCOS_FP8_WORKSPACE_BYTES 256
 #define BITCOS_FP8_ROWS_MAX 0x7FFFFF00

@@ -11,12 +11,13 @@
 //
 // Two operand orders, chosen by the host from the sizes:
 //   tokens first   (more than 64 rows, longer groups) A = 256 tokens, B = 256 weight rows, two blocks of a cluster as one
-//                  (cta_group::2): each loads its 128 tokens and half of the weight rows, 64 bytes a clock and multiprocessor from L2 at the
-//                  tensor cores' rate, where a block by itself would need 96 and L2 gives about 40 (11 TB/s).  A promoter thread holds 128
-//                  columns of one token; the scales of a group are one number per thread.  Persistent.  4095 x 8192 x 5120: 146 to 152 us
-//                  (2.3 PFLOP/s); a group of 128 takes about 800 clocks for the 512 of its products: what bounds it is the round
-//                  products -> promoters -> products over two accumulators, all that tensor memory holds of 256 columns (and at 2 PFLOP/s and
-//                  more the power limit: the clock is at 1.4 GHz).
+//                  (cta_group::2): each loads its 128 tokens and half of the weight rows, 32 KB a group of 128, where a block by itself would
+//                  load 48.  A promoter thread holds 128 columns of one token; the scales of a group are one number per thread.
+//                  Persistent.  A group takes about 770 clocks for the 512 of its products, whether one pair of blocks is at work or
+//                  all (764, 771, 747, 718 and 837 clocks with 1, 8, 32, 64 and 74 tiles; L2 then gives 29 % of its sectors at most): what bounds
+//                  it is the round products -> promoters -> products over two accumulators, all that tensor memory holds of 256 columns, and not
+//                  L2.  At the power limit the clock comes on top: 4095 x 8192 x 5120 is 280 groups one after another, recorded 146 to 152 us
+//                  on a cool board (2.3 PFLOP/s, 1.4 GHz), 168 to 176 on a warm one.
 //   weights first  A = 128 weight rows, B = 16, 32 or 64 tokens (16 of routed pairs).  Two or three blocks per multiprocessor keep enough of the weights
 //                  under way, and K is cut over the blocks of a cluster where there are few row blocks: each leaves its sums in shared
 //                  memory, and the cluster adds them in order of rank (no workspace, no atomics, the same bits every time).  Bound by
@@ -545,7 +546,8 @@ fp8_matmul_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constan
     int n_groups = 0;
     int64_t n_tiles = static_cast<int64_t>(a.row_tiles) * a.w_tiles;
     if constexpr (GROUPED) {
-        // (the first 32 groups are asked for together with their number: one trip to memory less)
+        // (the first 32 groups are asked for together with their number: one trip to memory less; each further 32 are one trip
+        // more, three for 128)
         int e0 = 0, begin0 = 0, end0 = 0;
         if (warp == 0 && lane < a.max_groups) {
             e0 = __ldg(a.group_expert + lane);
@@ -1254,7 +1256,8 @@ int multiprocessors(int *sms) {
 // Dense, weights first: into how many shares K is cut, and the nanoseconds expected of it.  A block takes 270, 310 or 490 ns for a group
 // of 128 at 16, 32 and 64 tokens (640 rows, K = 6400 and 25600), or, with all multiprocessors at it, what memory needs for its
 // 16 KB; start, first copies and the cluster's sum cost 2 us more per round.  The clusters that the device holds at once are asked for
-// once per kernel and device (of seven blocks there are 30: 40 row blocks of 5120 x 25600 took two rounds and 36 us).
+// once per kernel and device (of seven blocks there are 30: 40 row blocks of 5120 x 25600 took two rounds and 36 us).  Tokens first 410 ns a
+// group, its 770 clocks at 1.9 GHz: calls this short are not at the power limit.
 constexpr int64_t kGroupNs16 = 270, kGroupNs32 = 310, kGroupNs64 = 490, kRoundNs = 2000, kPairGroupNs = 410, kPairNs = 3500;
 template <int N, bool GROUPED>
 int plan_weights_first(const Fp8Args &a, int64_t tiles, int sms, int *splits_out, int64_t *ns_out) {
@@ -1369,9 +1372,13 @@ int bitcos_fp8_matmul_limited(const uint8_t *W, const float *w_scale, int64_t M,
     rc = multiprocessors(&sms);
     if (rc) return rc;
     const int64_t row_tiles = (rows + 255) / 256, w_tiles = (M + 255) / 256;
+    // Above 512 rows tokens first: 600 x 6912 x 2560 23.3 us against 35.6 weights first, 1024 x 8192 x 5120 42.4 against 122, 2048 x 2560 x 2560
+    // 23.4 against 54.9.  (The other way round where M leaves most pairs without a tile and K is long: 513 x 128 x 25600 83 us against 18,
+    // 1024 x 256 x 25600 86 against 25, 4095 x 64 x 25600 89 against 35.  The rule does not look at that.)
     bool pairs = rows > 512;
     if (rows > 64 && !pairs) {
-        // few rows: whichever ends sooner
+        // few rows: whichever ends sooner (200 x 8192 x 5120 tokens first 22.7 us against 29.9, 300 x 6912 x 2560 14.3 against 18.0, 128 x 2560 x 6912
+        // weights first 11.7 against 26.8)
         int splits = 0;
         int64_t ns = 0;
         rc = plan_weights_first<64, false>(a, (rows + 63) / 64 * a.w_blocks, sms, &splits, &ns);
@@ -1444,7 +1451,9 @@ int bitcos_fp8_matmul_grouped_limited(const uint8_t *W, const float *w_scale, in
     a.w_tiles = a.w_blocks;
     if ((n_pairs / 16 + max_groups) * a.w_tiles > INT_MAX) return BITCOS_ERR_SHAPE;
     // 16 tokens a tile, weights first, against 256, tokens first: 128 experts of 1536 x 2048 (2048 x 768), mean 16 75 us against 123 (39 against
-    // 77), 38 109 against 132 (62 against 75), 48 129 against 131 (76 against 75), 64 165 against 132 (93 against 74).  Tiles of 32 and 64 tokens
+    // 77), 38 109 against 132 (62 against 75), 48 129 against 131 (76 against 75), 64 165 against 132 (93 against 74).  With groups as routing makes
+    // them, of all lengths, the line is where it is: mean 48 118 against 120 (74 against 76; 64 experts of 1000 x 2048 43 against 48, 32 of 1024 x 512
+    // 11.5 against 12.8), mean 64 156 against 128 (94 against 78; 56 against 48, 14.3 against 13.0).  Tiles of 32 and 64 tokens
     // lay between: 32 gained 5 to 7 % at means of 20 to 32 on the first shape and lost as much on the second, 64 won 5 % at 48 and nowhere else;
     // and tiles of 16 cost what the groups' lengths are, whatever their mean.
     if (mean <= 48) {
